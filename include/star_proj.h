@@ -553,6 +553,138 @@ star_status star_attn_decode(const star_attn_shape *shape, const int32_t *pos_ty
                              const void *V_cache, star_dtype dt, void *O, star_dtype ot, void *ws,
                              size_t ws_bytes, hipStream_t stream);
 
+/*
+ * Attention over a pack: sequences of different lengths, one behind the other
+ * in T rows, causal within each (the same scores, laws and layouts as
+ * star_attn_fwd, with [T] in the place of [batch][seq_len]).  In these calls
+ * star_attn_shape holds
+ *   batch    the sequences of the pack
+ *   seq_len  T, the rows of all of them (at most STAR_PACK_MAX_TOKENS)
+ *
+ * The pack's plan is built once from the row types and the sequences' bounds,
+ * and serves every layer and both directions, for any heads, head width and
+ * law with that q:
+ *   row_type    device int32[T]: each row's type, as the projections take it.
+ *               A row whose type lies outside [0, q) is neither a query nor a
+ *               key.
+ *   cu_seqlens  device int32[batch + 1]: sequence s is rows cu_seqlens[s] ..
+ *               cu_seqlens[s + 1] - 1; none, one or many.  The bounds may not
+ *               decrease.  They are read on the device and cannot be refused:
+ *               bounds below an earlier one or outside [0, T] count as the
+ *               nearest that is allowed, so sequences never overlap and no
+ *               call reads or writes outside its buffers.
+ *   pack        device buffer of at least star_attn_pack_bytes(q, T, batch)
+ *               bytes, 16-byte aligned
+ * A call with a pack that was built for another T, batch or q writes nothing.
+ *
+ * Rows that no sequence holds (behind the last one) are left as they were, or
+ * with `clear_rest` written as zeros (lse: -infinity).  Rows of a type out of
+ * range are written as zeros either way.
+ *
+ * star_attn_packed_fwd: O [T][n_heads][head_dim]; lse float[n_heads][T] or
+ *   NULL (the gradient needs it).
+ * star_attn_packed_bwd: the gradients of Q, K and V for the gradient dO of O
+ *   (bf16), from the forward's O (dtype ot) and lse; those of a key/value head
+ *   are summed over its query heads.  With s the scaled scores,
+ *   P = exp(s - lse) and delta_p = <dO_p, O_p>:
+ *     dS_pu = P_pu (<dO_p, V_u> - delta_p),  dV_u = sum_p P_pu dO_p,
+ *     dQ_p^(a) = sum_u scale_pu dS_pu K_u^(a),
+ *     dK_u^(a) = sum_p scale_pu dS_pu Q_p^(a)   over the pairs with a in F.
+ *   dQ [T][n_heads][head_dim], dK and dV [T][n_kv_heads][head_dim] of dtype
+ *   gt.  P and dS enter their products rounded to bf16, sums are fp32, every
+ *   element has one order of summation.  ws: star_attn_packed_bwd_workspace_bytes
+ *   (shape) bytes.
+ * Errors as star_attn_fwd; STAR_ERR_WORKSPACE for a pack or ws that is too
+ * small; more than STAR_PACK_MAX_SEQS sequences: STAR_ERR_SHAPE.  The values
+ * must be finite: a NaN or an infinity may reach other rows of its sequence.
+ */
+#define STAR_PACK_MAX_TOKENS (1 << 18)
+#define STAR_PACK_MAX_SEQS (1 << 14)
+size_t star_attn_pack_bytes(int32_t q, int64_t T, int32_t batch);
+star_status star_attn_pack(int32_t q, int64_t T, int32_t batch, const int32_t *row_type,
+                           const int32_t *cu_seqlens, void *pack, size_t pack_bytes,
+                           hipStream_t stream);
+star_status star_attn_packed_fwd(const star_attn_shape *shape, const void *pack, size_t pack_bytes,
+                                 const void *Q, const void *K, const void *V, star_dtype dt, void *O,
+                                 star_dtype ot, float *lse, int32_t clear_rest, hipStream_t stream);
+size_t star_attn_packed_bwd_workspace_bytes(const star_attn_shape *shape);
+star_status star_attn_packed_bwd(const star_attn_shape *shape, const void *pack, size_t pack_bytes,
+                                 const void *dO, const void *Q, const void *K, const void *V,
+                                 star_dtype dt, const void *O, star_dtype ot, const float *lse,
+                                 void *dQ, void *dK, void *dV, star_dtype gt, int32_t clear_rest,
+                                 void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Paged key-value cache.  Keys and values live in pages of page_size
+ * positions, device [n_pages][n_kv_heads][page_size][head_dim] (a head's rows
+ * of a page are contiguous); position u of sequence b lies in page
+ * page_table[b][u / page_size].
+ *   type    STAR_KV_BF16, or 8 bits per element with a scale byte per row of a
+ *           head, device uint8 [n_pages][n_kv_heads][page_size] for K and V
+ *           each: STAR_KV_E4M3 (OCP e4m3) or STAR_KV_INT8.  A scale byte s
+ *           stands for 2^(s - 127); a row's values are its elements times
+ *           that.  s is the least (from 1 on) at which the row's largest
+ *           magnitude fits the type (448, 127), elements are rounded to
+ *           nearest even; a value read back is exact in bf16.  A row that
+ *           holds a NaN or an infinity gets s = 255 and reads back as NaN.
+ *   page_table  device int32 [batch][max_pages].  Entries behind a sequence's
+ *           length are not read.  An entry outside [0, n_pages) is a page that
+ *           is not there: its positions are neither written nor attended to
+ *           and read back as zeros.  Sequences may share pages to read; two
+ *           rows that one call writes to the same place leave it unspecified.
+ * head_dim 64 or 128, page_size a power of two from 8 to 1024, K, V, K_scale,
+ * V_scale 16-byte aligned (the scales are NULL for STAR_KV_BF16).
+ *
+ * star_kv_append writes the rows K, V (device [T][n_kv_heads][head_dim], bf16)
+ * of new tokens, packed by cu_seqlens (device int32[batch + 1], as above: a
+ * whole prompt, one token each, none), into the cache.  cache_len (device
+ * int32[batch]) is every sequence's length with them, as star_attn_decode_paged
+ * then takes it: token t of sequence b is position
+ * cache_len[b] - (cu_seqlens[b + 1] - t).  Tokens whose position is below 0 or
+ * beyond max_pages pages are left out.
+ * star_kv_read is the inverse: the same arguments, K and V are written (rows
+ * without an entry: zeros; rows outside every sequence: left as they were, or
+ * zeros with clear_rest).
+ */
+typedef enum { STAR_KV_BF16 = 0, STAR_KV_E4M3 = 1, STAR_KV_INT8 = 2 } star_kv_type;
+typedef struct {
+    int32_t n_pages;
+    int32_t page_size;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t batch;     /* sequences */
+    int32_t max_pages; /* per sequence */
+    star_kv_type type;
+    void *K;
+    void *V;
+    uint8_t *K_scale;
+    uint8_t *V_scale;
+    const int32_t *page_table;
+} star_kv_pages;
+
+star_status star_kv_append(const star_kv_pages *pages, const int32_t *cu_seqlens,
+                           const int32_t *cache_len, int64_t T, const void *K, const void *V,
+                           star_dtype dt, hipStream_t stream);
+star_status star_kv_read(const star_kv_pages *pages, const int32_t *cu_seqlens,
+                         const int32_t *cache_len, int64_t T, void *K, void *V, star_dtype dt,
+                         int32_t clear_rest, hipStream_t stream);
+
+/* star_attn_decode over a paged cache: one new query row per sequence against
+ * positions 0 .. cache_len[b] - 1, the last of which is its own.
+ *   shape    batch, n_kv_heads and head_dim as in pages; seq_len the capacity
+ *            max_pages * page_size
+ *   pos_type device int32[seq_len]; 16-byte aligned, like every pointer
+ *   cache_len, Q, O as in star_attn_decode; zero rows as there
+ *   ws       star_attn_decode_paged_workspace_bytes(shape) bytes
+ * The keys of all sequences are shared out evenly over the chip, long
+ * sequences split and joined again in a second launch; the result of a call
+ * depends on its arguments alone. */
+size_t star_attn_decode_paged_workspace_bytes(const star_attn_shape *shape);
+star_status star_attn_decode_paged(const star_attn_shape *shape, const star_kv_pages *pages,
+                                   const int32_t *pos_type, const int32_t *cache_len, const void *Q,
+                                   star_dtype dt, void *O, star_dtype ot, void *ws, size_t ws_bytes,
+                                   hipStream_t stream);
+
 /* Static description of a status code. */
 const char *star_status_string(star_status s);
 

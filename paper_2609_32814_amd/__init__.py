@@ -17,6 +17,9 @@ _EXPORTS = (
     "star_swiglu_ffn_bwd", "star_decode_gated", "star_decode_status", "star_decode_noalloc",
     "AttnShape", "star_attn_fwd", "star_attn_decode", "star_attn_decode_workspace_bytes",
     "star_set_fwd_tiles", "star_tile_shape", "star_swiglu_merged_fwd", "star_swiglu_up_fwd_planned", "pack_gate_up",
+    "star_attn_pack", "star_attn_pack_bytes", "star_attn_packed_fwd", "star_attn_packed_bwd",
+    "star_attn_packed_bwd_workspace_bytes", "KVPages", "star_kv_append", "star_kv_read", "star_attn_decode_paged",
+    "star_attn_decode_paged_workspace_bytes",
 )
 
 __all__ = list(_EXPORTS)

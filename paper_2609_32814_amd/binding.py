@@ -41,6 +41,13 @@ class _CAlgebra(ctypes.Structure):
                 ("edges", ctypes.POINTER(ctypes.c_uint8))]
 
 
+class _CKvPages(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("type", ctypes.c_int), ("K", ctypes.c_void_p), ("V", ctypes.c_void_p),
+                ("K_scale", ctypes.c_void_p), ("V_scale", ctypes.c_void_p), ("page_table", ctypes.c_void_p)]
+
+
 class _CAttnShape(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("seq_len", ctypes.c_int32), ("n_heads", ctypes.c_int32),
                 ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("q", ctypes.c_int32),
@@ -92,6 +99,19 @@ def _load() -> ctypes.CDLL:
     lib.star_attn_decode_workspace_bytes.argtypes = [S]
     lib.star_attn_decode_workspace_bytes.restype = sz
     lib.star_attn_decode.argtypes = [S, P, P, P, P, P, E, P, E, P, sz, P]
+    KV = ctypes.POINTER(_CKvPages)
+    lib.star_attn_pack_bytes.argtypes = [i32, i64, i32]
+    lib.star_attn_pack_bytes.restype = sz
+    lib.star_attn_pack.argtypes = [i32, i64, i32, P, P, P, sz, P]
+    lib.star_attn_packed_fwd.argtypes = [S, P, sz, P, P, P, E, P, E, P, i32, P]
+    lib.star_attn_packed_bwd_workspace_bytes.argtypes = [S]
+    lib.star_attn_packed_bwd_workspace_bytes.restype = sz
+    lib.star_attn_packed_bwd.argtypes = [S, P, sz, P, P, P, P, E, P, E, P, P, P, P, E, i32, P, sz, P]
+    lib.star_kv_append.argtypes = [KV, P, P, i64, P, P, E, P]
+    lib.star_kv_read.argtypes = [KV, P, P, i64, P, P, E, i32, P]
+    lib.star_attn_decode_paged_workspace_bytes.argtypes = [S]
+    lib.star_attn_decode_paged_workspace_bytes.restype = sz
+    lib.star_attn_decode_paged.argtypes = [S, KV, P, P, P, E, P, E, P, sz, P]
     lib.star_status_string.argtypes = [E]
     lib.star_status_string.restype = ctypes.c_char_p
     for name in ("star_proj_fwd", "star_proj_bwd_data", "star_proj_bwd_weight", "star_ffn_fwd",
@@ -100,7 +120,9 @@ def _load() -> ctypes.CDLL:
                  "star_proj_bwd_data_pair_planned", "star_tile_shape",
                  "star_proj_bwd_weight_planned", "star_swiglu_fwd", "star_swiglu_bwd", "star_add",
                  "star_decode_gated", "star_decode_status", "star_decode_noalloc", "star_attn_fwd",
-                 "star_attn_decode", "star_swiglu_merged_fwd", "star_swiglu_up_fwd_planned"):
+                 "star_attn_decode", "star_swiglu_merged_fwd", "star_swiglu_up_fwd_planned", "star_attn_pack",
+                 "star_attn_packed_fwd", "star_attn_packed_bwd", "star_kv_append", "star_kv_read",
+                 "star_attn_decode_paged"):
         getattr(lib, name).restype = E
     return lib
 
@@ -846,4 +868,213 @@ def star_attn_decode(shape: AttnShape, pos_type: torch.Tensor, cache_len: torch.
     _check(LIB.star_attn_decode(shape.ref, _ptr(pos_type), _ptr(cache_len), _ptr(Q), _ptr(K_cache),
                                 _ptr(V_cache), DTYPES[torch.bfloat16], _ptr(O), _dt(O), _ptr(ws),
                                 ws.numel() * ws.element_size(), _stream(dev)), "star_attn_decode")
+    return O
+
+
+# ---- attention over packs ------------------------------------------------------
+
+
+def star_attn_pack_bytes(q: int, T: int, n_seq: int) -> int:
+    return int(LIB.star_attn_pack_bytes(int(q), int(T), int(n_seq)))
+
+
+def star_attn_pack(q: int, row_type: torch.Tensor, cu_seqlens: torch.Tensor, pack=None) -> torch.Tensor:
+    """The plan of a pack (device uint8 buffer): sequence s is rows
+    ``cu_seqlens[s]`` .. ``cu_seqlens[s + 1] - 1`` of types ``row_type`` [T].
+    Built once per batch; every layer's forward and backward take it."""
+    dev = row_type.device
+    T, n = row_type.numel(), cu_seqlens.numel() - 1
+    _types(row_type, T, dev)
+    if n < 0:
+        raise ValueError("cu_seqlens needs one entry more than there are sequences")
+    _need(cu_seqlens, "cu_seqlens", (n + 1,), _I32, dev)
+    if pack is None:
+        pack = torch.empty(max(star_attn_pack_bytes(q, T, n), 16), dtype=torch.uint8, device=dev)
+    _need(pack, "pack", (pack.numel(),), (torch.uint8,), dev)
+    _gpu(dev)
+    _check(LIB.star_attn_pack(int(q), T, n, _ptr(row_type), _ptr(cu_seqlens), _ptr(pack), pack.numel(), _stream(dev)),
+           "star_attn_pack")
+    return pack
+
+
+def star_attn_packed_fwd(shape: AttnShape, pack: torch.Tensor, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
+                         O=None, out_dtype=torch.bfloat16, lse=None, want_lse: bool = False):
+    """Causal algebraic attention over a pack: ``shape.batch`` sequences in
+    ``shape.seq_len`` rows, Q [T, n_heads, d_h], K and V [T, n_kv_heads, d_h],
+    bf16; ``pack`` from ``star_attn_pack``.  Returns O (and the log-sum-exp
+    [n_heads, T] when ``want_lse`` or ``lse`` is given).  Rows outside every
+    sequence are left as they were in buffers of the caller's and are zeros
+    when this call allocates O."""
+    T, H, Hkv, D = shape.seq_len, shape.n_heads, shape.n_kv_heads, shape.head_dim
+    dev = Q.device if isinstance(Q, torch.Tensor) else None
+    _need(Q, "Q", (T, H, D), _BF16, dev)
+    _need(K, "K", (T, Hkv, D), _BF16, dev)
+    _need(V, "V", (T, Hkv, D), _BF16, dev)
+    _need(pack, "pack", (pack.numel(),), (torch.uint8,), dev)
+    clear = O is None
+    if O is None:
+        O = torch.empty((T, H, D), dtype=out_dtype, device=dev)
+    _need(O, "O", (T, H, D), _FLOATS, dev)
+    if lse is None and want_lse:
+        lse = torch.empty((H, T), dtype=torch.float32, device=dev)
+    _opt(lse, "lse", (H, T), _F32, dev)
+    _gpu(dev)
+    _check(LIB.star_attn_packed_fwd(shape.ref, _ptr(pack), pack.numel(), _ptr(Q), _ptr(K), _ptr(V),
+                                    DTYPES[torch.bfloat16], _ptr(O), _dt(O), _ptr(lse), int(clear), _stream(dev)),
+           "star_attn_packed_fwd")
+    return (O, lse) if lse is not None else O
+
+
+def star_attn_packed_bwd_workspace_bytes(shape: AttnShape) -> int:
+    return int(LIB.star_attn_packed_bwd_workspace_bytes(shape.ref))
+
+
+def star_attn_packed_bwd(shape: AttnShape, pack: torch.Tensor, dO: torch.Tensor, Q: torch.Tensor, K: torch.Tensor,
+                         V: torch.Tensor, O: torch.Tensor, lse: torch.Tensor, dQ=None, dK=None, dV=None,
+                         out_dtype=torch.bfloat16, ws=None):
+    """Gradients (dQ, dK, dV) of ``star_attn_packed_fwd`` for the gradient dO
+    [T, n_heads, d_h] (bf16) of its output, from that call's O and lse.  Give
+    all of dQ, dK, dV or none: rows outside every sequence are left as they
+    were in the caller's and zeros in those allocated here."""
+    T, H, Hkv, D = shape.seq_len, shape.n_heads, shape.n_kv_heads, shape.head_dim
+    dev = Q.device if isinstance(Q, torch.Tensor) else None
+    _need(dO, "dO", (T, H, D), _BF16, dev)
+    _need(Q, "Q", (T, H, D), _BF16, dev)
+    _need(K, "K", (T, Hkv, D), _BF16, dev)
+    _need(V, "V", (T, Hkv, D), _BF16, dev)
+    _need(O, "O", (T, H, D), _FLOATS, dev)
+    _need(lse, "lse", (H, T), _F32, dev)
+    _need(pack, "pack", (pack.numel(),), (torch.uint8,), dev)
+    given = [g is not None for g in (dQ, dK, dV)]
+    if any(given) and not all(given):
+        raise ValueError("give all of dQ, dK and dV, or none")
+    if not any(given):
+        dQ = torch.empty((T, H, D), dtype=out_dtype, device=dev)
+        dK = torch.empty((T, Hkv, D), dtype=out_dtype, device=dev)
+        dV = torch.empty((T, Hkv, D), dtype=out_dtype, device=dev)
+    _need(dQ, "dQ", (T, H, D), _FLOATS, dev)
+    _need(dK, "dK", (T, Hkv, D), (dQ.dtype,), dev)
+    _need(dV, "dV", (T, Hkv, D), (dQ.dtype,), dev)
+    if ws is None:
+        ws = torch.empty(max(star_attn_packed_bwd_workspace_bytes(shape), 16), dtype=torch.uint8, device=dev)
+    _need(ws, "ws", tuple(ws.shape), None, dev)
+    _gpu(dev)
+    _check(LIB.star_attn_packed_bwd(shape.ref, _ptr(pack), pack.numel(), _ptr(dO), _ptr(Q), _ptr(K), _ptr(V),
+                                    DTYPES[torch.bfloat16], _ptr(O), _dt(O), _ptr(lse), _ptr(dQ), _ptr(dK), _ptr(dV),
+                                    _dt(dQ), int(not any(given)), _ptr(ws), ws.numel() * ws.element_size(),
+                                    _stream(dev)), "star_attn_packed_bwd")
+    return dQ, dK, dV
+
+
+# ---- paged key-value cache -----------------------------------------------------
+
+KV_TYPES = {torch.bfloat16: 0, torch.float8_e4m3fn: 1, torch.int8: 2}
+
+
+class KVPages:
+    """A paged key-value cache: K_pages and V_pages [n_pages, n_kv_heads,
+    page_size, d_h] of bfloat16, float8_e4m3fn or int8, page_table
+    [sequences, max_pages] (int32), and for the 8-bit types the scale bytes
+    K_scale and V_scale [n_pages, n_kv_heads, page_size] (uint8).  The tensors
+    stay the caller's: a page table written in place is seen by the next call."""
+
+    def __init__(self, K_pages: torch.Tensor, V_pages: torch.Tensor, page_table: torch.Tensor, K_scale=None,
+                 V_scale=None):
+        if not isinstance(K_pages, torch.Tensor) or K_pages.dim() != 4:
+            raise ValueError("K_pages must be [n_pages, n_kv_heads, page_size, head_dim]")
+        if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+            raise ValueError("page_table must be [sequences, max_pages]")
+        dev = K_pages.device
+        shape = tuple(K_pages.shape)
+        _need(K_pages, "K_pages", shape, tuple(KV_TYPES), dev)
+        _need(V_pages, "V_pages", shape, (K_pages.dtype,), dev)
+        _need(page_table, "page_table", tuple(page_table.shape), _I32, dev)
+        if K_pages.dtype == torch.bfloat16:
+            if K_scale is not None or V_scale is not None:
+                raise ValueError("bfloat16 pages take no scales")
+        else:
+            _need(K_scale, "K_scale", shape[:3], (torch.uint8,), dev)
+            _need(V_scale, "V_scale", shape[:3], (torch.uint8,), dev)
+        self.K_pages, self.V_pages, self.page_table = K_pages, V_pages, page_table
+        self.K_scale, self.V_scale = K_scale, V_scale
+        self.device, self.batch, self.max_pages = dev, page_table.shape[0], page_table.shape[1]
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = shape
+        self._c = _CKvPages(self.n_pages, self.page_size, self.n_kv_heads, self.head_dim, self.batch, self.max_pages,
+                            KV_TYPES[K_pages.dtype], _ptr(K_pages), _ptr(V_pages), _ptr(K_scale), _ptr(V_scale),
+                            _ptr(page_table))
+        self.ref = ctypes.byref(self._c)
+
+    @property
+    def capacity(self) -> int:
+        """Positions per sequence."""
+        return self.max_pages * self.page_size
+
+    def __repr__(self):
+        return (f"KVPages({self.n_pages} x {self.page_size} positions, n_kv_heads={self.n_kv_heads}, "
+                f"head_dim={self.head_dim}, {self.K_pages.dtype}, batch={self.batch}, max_pages={self.max_pages})")
+
+
+def _kv_rows(pages: KVPages, cu_seqlens, cache_len):
+    dev = pages.device
+    _need(cu_seqlens, "cu_seqlens", (pages.batch + 1,), _I32, dev)
+    _need(cache_len, "cache_len", (pages.batch,), _I32, dev)
+    _gpu(dev)
+    return dev
+
+
+def star_kv_append(pages: KVPages, cu_seqlens: torch.Tensor, cache_len: torch.Tensor, K: torch.Tensor, V: torch.Tensor):
+    """Writes the keys and values K, V [T, n_kv_heads, d_h] (bf16) of new
+    tokens into the cache, quantised where its pages are 8 bits.  Sequence b's
+    tokens are rows ``cu_seqlens[b]`` .. ``cu_seqlens[b + 1] - 1``, its last
+    positions below ``cache_len[b]`` (the length with them)."""
+    T = K.shape[0] if isinstance(K, torch.Tensor) and K.dim() == 3 else -1
+    dev = _kv_rows(pages, cu_seqlens, cache_len)
+    _need(K, "K", (T, pages.n_kv_heads, pages.head_dim), _BF16, dev)
+    _need(V, "V", (T, pages.n_kv_heads, pages.head_dim), _BF16, dev)
+    _check(LIB.star_kv_append(pages.ref, _ptr(cu_seqlens), _ptr(cache_len), T, _ptr(K), _ptr(V),
+                              DTYPES[torch.bfloat16], _stream(dev)), "star_kv_append")
+
+
+def star_kv_read(pages: KVPages, cu_seqlens: torch.Tensor, cache_len: torch.Tensor, T: int, K=None, V=None):
+    """The inverse of ``star_kv_append``: (K, V) [T, n_kv_heads, d_h] in bf16,
+    read back from the cache (exact).  Rows without an entry are zeros; rows
+    outside every sequence are left as they were in the caller's K and V and
+    zeros in those allocated here."""
+    dev = _kv_rows(pages, cu_seqlens, cache_len)
+    if (K is None) != (V is None):
+        raise ValueError("give both of K and V, or none")
+    clear = K is None
+    if clear:
+        K, V = (torch.empty((int(T), pages.n_kv_heads, pages.head_dim), dtype=torch.bfloat16, device=dev)
+                for _ in range(2))
+    _need(K, "K", (int(T), pages.n_kv_heads, pages.head_dim), _BF16, dev)
+    _need(V, "V", (int(T), pages.n_kv_heads, pages.head_dim), _BF16, dev)
+    _check(LIB.star_kv_read(pages.ref, _ptr(cu_seqlens), _ptr(cache_len), int(T), _ptr(K), _ptr(V),
+                            DTYPES[torch.bfloat16], int(clear), _stream(dev)), "star_kv_read")
+    return K, V
+
+
+def star_attn_decode_paged_workspace_bytes(shape: AttnShape) -> int:
+    return int(LIB.star_attn_decode_paged_workspace_bytes(shape.ref))
+
+
+def star_attn_decode_paged(shape: AttnShape, pages: KVPages, pos_type: torch.Tensor, cache_len: torch.Tensor,
+                           Q: torch.Tensor, O=None, out_dtype=torch.bfloat16, ws=None):
+    """One decode step over a paged cache: ``star_attn_decode`` with the keys
+    and values in ``pages`` (``shape.seq_len`` is ``pages.capacity``)."""
+    B, S, H, D = shape.batch, shape.seq_len, shape.n_heads, shape.head_dim
+    dev = pages.device
+    _need(Q, "Q", (B, H, D), _BF16, dev)
+    _need(pos_type, "pos_type", (S,), _I32, dev)
+    _need(cache_len, "cache_len", (B,), _I32, dev)
+    if O is None:
+        O = torch.empty((B, H, D), dtype=out_dtype, device=dev)
+    _need(O, "O", (B, H, D), _FLOATS, dev)
+    _gpu(dev)
+    if ws is None:
+        ws = torch.empty(max(star_attn_decode_paged_workspace_bytes(shape), 16), dtype=torch.uint8, device=dev)
+    _need(ws, "ws", tuple(ws.shape), None, dev)
+    _check(LIB.star_attn_decode_paged(shape.ref, pages.ref, _ptr(pos_type), _ptr(cache_len), _ptr(Q),
+                                      DTYPES[torch.bfloat16], _ptr(O), _dt(O), _ptr(ws),
+                                      ws.numel() * ws.element_size(), _stream(dev)), "star_attn_decode_paged")
     return O

@@ -18,7 +18,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libstarq.so")
-SOURCES = ["plan.hip", "gemm.hip", "gemm_async.hip", "gemm_async_many.hip", "gemm_narrow.hip", "colsum.hip", "swiglu.hip", "decode.hip", "decode_stack.hip", "graph_fill.hip", "scratch.hip", "attention.hip", "api.cpp"]
+SOURCES = ["plan.hip", "gemm.hip", "gemm_async.hip", "gemm_async_many.hip", "gemm_narrow.hip", "colsum.hip", "swiglu.hip", "decode.hip", "decode_stack.hip", "graph_fill.hip", "scratch.hip", "attention.hip", "attn_pack.hip", "attn_bwd.hip",
+           "attn_paged.hip", "kv_pages.hip", "api.cpp"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [
@@ -43,6 +44,8 @@ def hipcc() -> str:
 # does the same: its tiles are a few K steps long, so the epilogue's reads
 # of the accumulators are a large share of its instructions.
 EXTRA_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "attn_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "attn_paged.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "gemm_narrow.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 

@@ -1690,4 +1690,254 @@ star_status star_attn_decode(const star_attn_shape* shape, const int32_t* pos_ty
   return hip_status(launch_attn_decode(p, stream));
 }
 
+// ---- attention over packs, the paged cache ----------------------------------
+
+extern "C++" {
+namespace {
+
+static_assert(STAR_PACK_MAX_TOKENS == kPackMaxTokens && STAR_PACK_MAX_SEQS == kPackMaxSeqs, "one limit for the ABI and the kernels");
+
+struct PackWs {
+  int32_t max_items = 0;
+  size_t perm = 0, mark = 0, recs_q = 0, recs_k = 0, raw_q = 0, raw_k = 0, key_q = 0, key_k = 0, end = 0;
+};
+star_status pack_layout(int32_t q, int64_t T, int32_t n_seq, PackWs& w) {
+  if (q < 1 || q > kAttnMaxQ) return STAR_ERR_ARG;
+  if (T < 0 || n_seq < 0 || T > kPackMaxTokens || n_seq > kPackMaxSeqs) return STAR_ERR_SHAPE;
+  w.max_items = pack_raw_base(T, n_seq, q);
+  const size_t recs = align_up(sizeof(int32_t) * pack_rec_ints(q) * static_cast<size_t>(w.max_items));
+  const size_t keys = align_up(sizeof(int32_t) * static_cast<size_t>(w.max_items));
+  w.perm = kAlign;  // behind the head
+  w.mark = w.perm + align_up(sizeof(int32_t) * T);
+  w.recs_q = w.mark + align_up(T);
+  w.recs_k = w.recs_q + recs;
+  w.raw_q = w.recs_k + recs;
+  w.raw_k = w.raw_q + recs;
+  w.key_q = w.raw_k + recs;
+  w.key_k = w.key_q + keys;
+  w.end = w.key_k + keys;
+  return STAR_OK;
+}
+PackView pack_view(const void* buf, const PackWs& w) {
+  void* p = const_cast<void*>(buf);
+  return {at<int32_t>(p, 0),        at<int32_t>(p, w.perm),  at<uint8_t>(p, w.mark),
+          at<int32_t>(p, w.recs_q), at<int32_t>(p, w.recs_k), at<int32_t>(p, w.raw_q),
+          at<int32_t>(p, w.raw_k),  at<int32_t>(p, w.key_q), at<int32_t>(p, w.key_k)};
+}
+
+star_status parse_pages(const star_kv_pages* pg, KvPages& kv) {
+  if (!pg) return STAR_ERR_ARG;
+  if (pg->type != STAR_KV_BF16 && pg->type != STAR_KV_E4M3 && pg->type != STAR_KV_INT8) return STAR_ERR_ARG;
+  if (pg->head_dim != 64 && pg->head_dim != 128) return STAR_ERR_UNSUPPORTED;
+  if (pg->page_size < 8 || pg->page_size > 1024 || (pg->page_size & (pg->page_size - 1))) return STAR_ERR_UNSUPPORTED;
+  if (pg->n_pages < 0 || pg->batch < 0 || pg->max_pages < 0 || pg->n_kv_heads < 1) return STAR_ERR_SHAPE;
+  if (static_cast<int64_t>(pg->max_pages) * pg->page_size > kKvMaxCapacity) return STAR_ERR_SHAPE;
+  int32_t shift = 0;
+  while ((1 << shift) < pg->page_size) ++shift;
+  kv = {pg->K,       pg->V, pg->K_scale,    pg->V_scale,  pg->page_table, pg->n_pages,
+        shift,       pg->n_kv_heads, pg->head_dim, pg->batch, pg->max_pages, static_cast<int32_t>(pg->type)};
+  return STAR_OK;
+}
+// the pointers of a cache that is to be used
+star_status check_pages(const KvPages& kv) {
+  if (!kv.table && kv.max_pages > 0) return STAR_ERR_ARG;
+  if (kv.n_pages > 0) {
+    if (!kv.K || !kv.V) return STAR_ERR_ARG;
+    if (kv.type != kKvBf16 && (!kv.k_scale || !kv.v_scale)) return STAR_ERR_ARG;
+  }
+  if (!aligned4(kv.table) || !aligned16(kv.K) || !aligned16(kv.V)) return STAR_ERR_ALIGN;
+  if (kv.type != kKvBf16 && (!aligned16(kv.k_scale) || !aligned16(kv.v_scale))) return STAR_ERR_ALIGN;
+  return STAR_OK;
+}
+star_status check_rows(const KvPages& kv, int64_t T, const int32_t* cu, const int32_t* cache_len, const void* K,
+                       const void* V, star_dtype dt) {
+  if (dt != STAR_BF16) return STAR_ERR_DTYPE;
+  // a thread per 8 elements, in one grid
+  if (T < 0 || T > 0x7fffffff || T * kv.n_kv > (int64_t{1} << 34)) return STAR_ERR_SHAPE;
+  if (T == 0) return STAR_OK;
+  if (!cu || !cache_len || !K || !V) return STAR_ERR_ARG;
+  if (!aligned4(cu) || !aligned4(cache_len) || !aligned16(K) || !aligned16(V)) return STAR_ERR_ALIGN;
+  return check_pages(kv);
+}
+
+struct PagedWs {
+  int32_t wgs = 0;
+  size_t part_o = 0, part_ml = 0, end = 0;
+};
+PagedWs paged_layout(const AttnShape& a) {
+  PagedWs w;
+  const int32_t rep = a.H / a.Hkv;
+  w.wgs = paged_workgroups(cu_count());
+  const size_t slots = (static_cast<size_t>(a.B) * a.Hkv * paged_groups(rep) + w.wgs) * paged_slice(rep);
+  w.part_o = 0;
+  w.part_ml = align_up(sizeof(float) * slots * a.D);
+  w.end = align_up(w.part_ml + sizeof(float) * 2 * slots);
+  return w;
+}
+}  // namespace
+}  // extern "C++"
+
+size_t star_attn_pack_bytes(int32_t q, int64_t T, int32_t batch) {
+  PackWs w;
+  return pack_layout(q, T, batch, w) == STAR_OK ? w.end : 0;
+}
+
+star_status star_attn_pack(int32_t q, int64_t T, int32_t batch, const int32_t* row_type, const int32_t* cu_seqlens,
+                           void* pack, size_t pack_bytes, hipStream_t stream) {
+  PackWs w;
+  star_status st = pack_layout(q, T, batch, w);
+  if (st != STAR_OK) return st;
+  if ((T > 0 && !row_type) || (batch > 0 && !cu_seqlens)) return STAR_ERR_ARG;
+  if (!pack || pack_bytes < w.end) return STAR_ERR_WORKSPACE;
+  if (!aligned16(pack) || !aligned4(row_type) || !aligned4(cu_seqlens)) return STAR_ERR_ALIGN;
+  return hip_status(launch_attn_pack(row_type, cu_seqlens, static_cast<int32_t>(T), batch, q, pack_view(pack, w), stream));
+}
+
+star_status star_attn_packed_fwd(const star_attn_shape* shape, const void* pack, size_t pack_bytes, const void* Q,
+                                 const void* K, const void* V, star_dtype dt, void* O, star_dtype ot, float* lse,
+                                 int32_t clear_rest, hipStream_t stream) {
+  AttnShape a;
+  star_status st = parse_attn(shape, a);
+  if (st != STAR_OK) return st;
+  PackWs w;
+  st = pack_layout(a.q, a.S, a.B, w);
+  if (st != STAR_OK) return st;
+  if (dt != STAR_BF16 || !valid_dtype(ot)) return STAR_ERR_DTYPE;
+  if (a.S == 0) return STAR_OK;
+  if (!Q || !K || !V || !O) return STAR_ERR_ARG;
+  if (!pack || pack_bytes < w.end) return STAR_ERR_WORKSPACE;
+  if (!aligned16(pack) || !aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O)) return STAR_ERR_ALIGN;
+  if (lse && !aligned4(lse)) return STAR_ERR_ALIGN;
+  const int64_t wgs = pack_main_wgs(a.H, w.max_items);
+  if (wgs + pack_clear_wgs(a.S) > 0x7fffff) return STAR_ERR_SHAPE;
+  AttnParams p = attn_params(a);
+  p.Q = Q;
+  p.K = K;
+  p.V = V;
+  p.O = O;
+  p.odtype = ot == STAR_BF16 ? 1 : 0;
+  p.lse = lse;
+  p.pack = pack_view(pack, w);
+  p.main_wgs = static_cast<int32_t>(wgs);
+  p.clear_rest = clear_rest;
+  return hip_status(launch_attn_packed_fwd(p, stream));
+}
+
+size_t star_attn_packed_bwd_workspace_bytes(const star_attn_shape* shape) {
+  AttnShape a;
+  if (parse_attn(shape, a) != STAR_OK || a.S > kPackMaxTokens) return 0;
+  return align_up(sizeof(float) * a.H * static_cast<size_t>(a.S));
+}
+
+star_status star_attn_packed_bwd(const star_attn_shape* shape, const void* pack, size_t pack_bytes, const void* dO,
+                                 const void* Q, const void* K, const void* V, star_dtype dt, const void* O,
+                                 star_dtype ot, const float* lse, void* dQ, void* dK, void* dV, star_dtype gt,
+                                 int32_t clear_rest, void* ws, size_t ws_bytes, hipStream_t stream) {
+  AttnShape a;
+  star_status st = parse_attn(shape, a);
+  if (st != STAR_OK) return st;
+  PackWs w;
+  st = pack_layout(a.q, a.S, a.B, w);
+  if (st != STAR_OK) return st;
+  if (dt != STAR_BF16 || !valid_dtype(ot) || !valid_dtype(gt)) return STAR_ERR_DTYPE;
+  if (a.S == 0) return STAR_OK;
+  if (!dO || !Q || !K || !V || !O || !lse || !dQ || !dK || !dV) return STAR_ERR_ARG;
+  if (!pack || pack_bytes < w.end || !ws || ws_bytes < star_attn_packed_bwd_workspace_bytes(shape)) return STAR_ERR_WORKSPACE;
+  for (const void* v : {pack, dO, Q, K, V, O, static_cast<const void*>(dQ), static_cast<const void*>(dK),
+                        static_cast<const void*>(dV), static_cast<const void*>(ws)})
+    if (!aligned16(v)) return STAR_ERR_ALIGN;
+  if (!aligned4(lse)) return STAR_ERR_ALIGN;
+  const int64_t q_wgs = pack_main_wgs(a.H, w.max_items), k_wgs = pack_main_wgs(a.Hkv, w.max_items);
+  if (q_wgs + pack_clear_wgs(a.S) > 0x7fffff) return STAR_ERR_SHAPE;
+  AttnBwdParams p{};
+  p.dO = dO;
+  p.Q = Q;
+  p.K = K;
+  p.V = V;
+  p.O = O;
+  p.lse = lse;
+  p.delta = static_cast<float*>(ws);
+  p.dQ = dQ;
+  p.dK = dK;
+  p.dV = dV;
+  p.odtype = ot == STAR_BF16 ? 1 : 0;
+  p.gdtype = gt == STAR_BF16 ? 1 : 0;
+  p.T = a.S;
+  p.n_seq = a.B;
+  p.n_heads = a.H;
+  p.n_kv = a.Hkv;
+  p.head_dim = a.D;
+  p.q = a.q;
+  p.law = a.law;
+  p.pack = pack_view(pack, w);
+  p.q_wgs = static_cast<int32_t>(q_wgs);
+  p.k_wgs = static_cast<int32_t>(k_wgs);
+  p.clear_rest = clear_rest;
+  return hip_status(launch_attn_packed_bwd(p, stream));
+}
+
+star_status star_kv_append(const star_kv_pages* pages, const int32_t* cu_seqlens, const int32_t* cache_len, int64_t T,
+                           const void* K, const void* V, star_dtype dt, hipStream_t stream) {
+  KvPages kv;
+  star_status st = parse_pages(pages, kv);
+  if (st != STAR_OK) return st;
+  st = check_rows(kv, T, cu_seqlens, cache_len, K, V, dt);
+  if (st != STAR_OK || T == 0 || kv.B == 0) return st;
+  return hip_status(launch_kv_append(kv, cu_seqlens, cache_len, static_cast<int32_t>(T), K, V, stream));
+}
+
+star_status star_kv_read(const star_kv_pages* pages, const int32_t* cu_seqlens, const int32_t* cache_len, int64_t T,
+                         void* K, void* V, star_dtype dt, int32_t clear_rest, hipStream_t stream) {
+  KvPages kv;
+  star_status st = parse_pages(pages, kv);
+  if (st != STAR_OK) return st;
+  st = check_rows(kv, T, cu_seqlens, cache_len, K, V, dt);
+  if (st != STAR_OK || T == 0) return st;
+  return hip_status(launch_kv_read(kv, cu_seqlens, cache_len, static_cast<int32_t>(T), K, V, clear_rest, stream));
+}
+
+size_t star_attn_decode_paged_workspace_bytes(const star_attn_shape* shape) {
+  AttnShape a;
+  if (parse_attn(shape, a) != STAR_OK) return 0;
+  return paged_layout(a).end;
+}
+
+star_status star_attn_decode_paged(const star_attn_shape* shape, const star_kv_pages* pages, const int32_t* pos_type,
+                                   const int32_t* cache_len, const void* Q, star_dtype dt, void* O, star_dtype ot,
+                                   void* ws, size_t ws_bytes, hipStream_t stream) {
+  AttnShape a;
+  star_status st = parse_attn(shape, a);
+  if (st != STAR_OK) return st;
+  AttnPagedParams p{};
+  st = parse_pages(pages, p.kv);
+  if (st != STAR_OK) return st;
+  if (dt != STAR_BF16 || !valid_dtype(ot)) return STAR_ERR_DTYPE;
+  if (p.kv.B != a.B || p.kv.n_kv != a.Hkv || p.kv.head_dim != a.D || (p.kv.max_pages << p.kv.page_shift) != a.S)
+    return STAR_ERR_SHAPE;
+  if (a.B == 0) return STAR_OK;
+  if (a.S == 0) return STAR_ERR_SHAPE;  // a decode step needs a cache
+  if (static_cast<int64_t>(a.B) * a.H > 0x7fffff) return STAR_ERR_SHAPE;
+  if (!pos_type || !cache_len || !Q || !O) return STAR_ERR_ARG;
+  st = check_pages(p.kv);
+  if (st != STAR_OK) return st;
+  if (!aligned16(pos_type) || !aligned4(cache_len) || !aligned16(Q) || !aligned16(O)) return STAR_ERR_ALIGN;
+  const PagedWs w = paged_layout(a);
+  if (!ws || ws_bytes < w.end) return STAR_ERR_WORKSPACE;
+  if (!aligned16(ws)) return STAR_ERR_ALIGN;
+  p.Q = Q;
+  p.pos_type = pos_type;
+  p.cache_len = cache_len;
+  p.O = O;
+  p.odtype = ot == STAR_BF16 ? 1 : 0;
+  p.cap = a.S;
+  p.n_heads = a.H;
+  p.q = a.q;
+  p.law = a.law;
+  p.groups = paged_groups(a.H / a.Hkv);
+  p.wgs = w.wgs;
+  p.part_o = at<float>(ws, w.part_o);
+  p.part_ml = at<float>(ws, w.part_ml);
+  return hip_status(launch_attn_decode_paged(p, stream));
+}
+
 }  // extern "C"

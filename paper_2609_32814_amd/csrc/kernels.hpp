@@ -260,6 +260,49 @@ hipError_t launch_decode_phase(const DecodePhase& p, hipStream_t stream);
 // token-major: Q and O [B][S][n_heads][head_dim], K and V
 // [B][S][n_kv][head_dim] (bf16), query head h reads key/value head
 // h / (n_heads / n_kv).
+
+// The plan of a pack: n_seq sequences of different lengths, one behind the
+// other in T rows, their tokens sorted by (sequence, type, position).  A work
+// item is a block of up to kAttnBlockRows tokens of one type of one sequence.
+// Its record holds what its walk reads: pack_rec_ints(q) words
+//   [0] first row of the sequence   [1] its length
+//   [2] perm index of the block     [3] type | tokens of the block << 16
+//   [4 + j], [4 + q + j]: perm index and count of the type-j tokens walked
+// (recs_q, a block of queries: the keys up to its last query; recs_k, a block
+// of keys: the queries from its first key on).  Each list is sorted by the
+// longest walk first.  starts and counts are sanitised by the kernel that
+// builds the plan, so no reader goes out of the T rows, whatever the caller's
+// sequence bounds hold.
+constexpr int kAttnBlockRows = 128;
+constexpr int kAttnMaxQ = 16;  // head_dim 128 in groups of 8
+constexpr int32_t kPackMaxTokens = 1 << 18;
+constexpr int32_t kPackMaxSeqs = 1 << 14;
+constexpr int32_t kPackMagic = 0x5041434b;
+struct PackView {
+  int32_t* head;   // [0] magic, [1] T, [2] n_seq, [3] q, [4] items
+  int32_t* perm;   // [T] positions within their sequence
+  uint8_t* mark;   // [T] 1: a token; 0: its type is out of range; 2: outside every sequence
+  int32_t* recs_q;
+  int32_t* recs_k;
+  int32_t* raw_q;  // the same before they are sorted, -1 in word 3 of the unused ones
+  int32_t* raw_k;
+  int32_t* key_q;  // what they are sorted by, per raw record
+  int32_t* key_k;
+};
+#ifdef __HIPCC__
+#define STARQ_HD __host__ __device__
+#else
+#define STARQ_HD
+#endif
+STARQ_HD inline int32_t pack_rec_ints(int32_t q) { return 4 + 2 * q; }
+// First raw record of a sequence that starts at row `start` with `s` sequences
+// before it: every type of every sequence ends in at most one partial block.
+STARQ_HD inline int32_t pack_raw_base(int64_t start, int64_t s, int64_t q) {
+  return static_cast<int32_t>((start + (kAttnBlockRows - 1) * q * s) / kAttnBlockRows);
+}
+hipError_t launch_attn_pack(const int32_t* types, const int32_t* cu, int32_t T, int32_t n_seq, int32_t q, const PackView& pack,
+                            hipStream_t stream);
+
 struct AttnParams {
   const void* Q;
   const void* K;
@@ -272,6 +315,10 @@ struct AttnParams {
   const int32_t* perm;
   const int32_t* offsets;
   int32_t items_per_bh;  // grid = B * n_heads * items_per_bh
+  // packed: B sequences, S rows in all
+  PackView pack;
+  int32_t main_wgs;    // workgroups of the work items; the others clear rows
+  int32_t clear_rest;  // rows outside every sequence are written as zeros
   // decode: S is the cache capacity; one query row per sequence
   const int32_t* pos_type;   // [S]
   const int32_t* cache_len;  // [B]
@@ -285,10 +332,96 @@ constexpr int32_t kAttnFwdMaxSeq = 1 << 18;  // positions per sequence in the fo
 // Forward work items per (sequence, head): 128-row query blocks over all types.
 inline int32_t attn_fwd_items(int32_t S, int32_t q) { return (S + 127 * q) / 128; }
 hipError_t launch_attn_fwd(const AttnParams& p, hipStream_t stream);
+hipError_t launch_attn_packed_fwd(const AttnParams& p, hipStream_t stream);
+
+// Gradient of the packed forward: dQ and delta first, then dK and dV.
+struct AttnBwdParams {
+  const void* dO;
+  const void* Q;
+  const void* K;
+  const void* V;
+  const void* O;
+  const float* lse;  // [n_heads][T]
+  float* delta;      // [n_heads][T]: <dO, O> of every row
+  void* dQ;
+  void* dK;
+  void* dV;
+  int32_t odtype, gdtype;  // of O and of the gradients: 0 fp32, 1 bf16
+  int32_t T, n_seq, n_heads, n_kv, head_dim, q, law;
+  PackView pack;
+  int32_t q_wgs, k_wgs;  // workgroups of the work items of either launch
+  int32_t clear_rest;
+};
+hipError_t launch_attn_packed_bwd(const AttnBwdParams& p, hipStream_t stream);
+
+// Work items of a pack by head.  Workgroup w runs on XCD w % 8.  An XCD takes
+// `per_xcd` units of the heads cut into `cuts` shares each (as many as it
+// takes for 8 to divide them), so that the query heads of one key/value head
+// sit on one XCD and read its keys and values through one L2, and every XCD
+// has equal numbers of long and short items.
+struct PackGrid {
+  int32_t cuts, per_xcd;
+};
+STARQ_HD inline PackGrid pack_grid(int32_t heads) {
+  const int32_t even = heads & -heads;
+  const int32_t cuts = even >= 8 ? 1 : 8 / even;
+  return {cuts, heads * cuts / 8};
+}
+inline int64_t pack_main_wgs(int32_t heads, int32_t max_items) {
+  const PackGrid g = pack_grid(heads);
+  return int64_t{8} * g.per_xcd * ((max_items + g.cuts - 1) / g.cuts);
+}
+constexpr int32_t kPackClearRows = 256;
+inline int64_t pack_clear_wgs(int32_t T) { return (T + kPackClearRows - 1) / kPackClearRows; }
+
 // Keys per decode split for a shape (a multiple of the 4 keys per team of
 // one batch; the same for every call with that shape).
 int32_t attn_decode_chunk(int32_t head_dim, int32_t batch, int32_t n_kv, int32_t head_groups, int32_t S);
 hipError_t launch_attn_decode(const AttnParams& p, hipStream_t stream);
+
+// ---- paged key-value cache -----------------------------------------------------
+
+// Pages [n_pages][n_kv][page][head_dim] of bf16, e4m3 or int8; the 8-bit types
+// with a scale byte b per row of a head, [n_pages][n_kv][page]: the row's
+// values are its elements times 2^(b - 127), NaN for b = 255.  Position u of
+// sequence b lies in page table[b][u / page].
+enum KvType : int { kKvBf16 = 0, kKvE4m3 = 1, kKvInt8 = 2 };
+struct KvPages {
+  void* K;
+  void* V;
+  uint8_t* k_scale;
+  uint8_t* v_scale;
+  const int32_t* table;  // [B][max_pages]
+  int32_t n_pages, page_shift, n_kv, head_dim, B, max_pages, type;
+};
+constexpr int32_t kKvMaxCapacity = 1 << 30;  // positions per sequence
+
+// Token t of sequence b (cu[b] <= t < cu[b + 1]) is position
+// cache_len[b] - (cu[b + 1] - t).  K, V [T][n_kv][head_dim] bf16.
+hipError_t launch_kv_append(const KvPages& kv, const int32_t* cu, const int32_t* cache_len, int32_t T, const void* K,
+                            const void* V, hipStream_t stream);
+hipError_t launch_kv_read(const KvPages& kv, const int32_t* cu, const int32_t* cache_len, int32_t T, void* K, void* V,
+                          int32_t clear_rest, hipStream_t stream);
+
+struct AttnPagedParams {
+  KvPages kv;
+  const void* Q;             // [B][n_heads][head_dim] bf16
+  const int32_t* pos_type;   // [cap]
+  const int32_t* cache_len;  // [B]
+  void* O;
+  int32_t odtype;
+  int32_t cap;               // max_pages pages
+  int32_t n_heads, q, law;
+  int32_t groups;            // slices of kPagedHeads query heads per key/value head
+  int32_t wgs;               // workgroups that share the tiles
+  float* part_o;             // [wgs + B n_kv groups][heads of a slice][head_dim]
+  float* part_ml;            // [...][heads of a slice][2]: maximum (base 2), sum
+};
+constexpr int kPagedHeads = 16;  // query heads per workgroup (the columns of a 16 x 16 product)
+STARQ_HD inline int32_t paged_groups(int32_t rep) { return (rep + kPagedHeads - 1) / kPagedHeads; }
+STARQ_HD inline int32_t paged_slice(int32_t rep) { return rep < kPagedHeads ? rep : kPagedHeads; }
+int32_t paged_workgroups(int cus);
+hipError_t launch_attn_decode_paged(const AttnPagedParams& p, hipStream_t stream);
 
 // The static workspace of star_decode_noalloc (scratch.hip): its size, and
 // its device address on the current device (looked up on the first call per
