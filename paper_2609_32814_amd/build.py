@@ -18,7 +18,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libstarq.so")
-SOURCES = ["plan.hip", "gemm.hip", "gemm_async.hip", "gemm_async_many.hip", "gemm_narrow.hip", "colsum.hip", "swiglu.hip", "decode.hip", "decode_stack.hip", "graph_fill.hip", "scratch.hip", "attention.hip", "attn_pack.hip", "attn_bwd.hip",
+SOURCES = ["plan.hip", "gemm.hip", "gemm_async.hip", "gemm_async_many.hip", "gemm_narrow.hip", "colsum.hip", "swiglu.hip", "decode.hip", "decode_stack.hip", "graph_fill.hip", "scratch.hip", "attention.hip", "attn_pack.hip", "attn_packed.hip", "attn_bwd.hip",
            "attn_paged.hip", "kv_pages.hip", "api.cpp"]
 ARCH = "gfx950"
 
@@ -44,6 +44,7 @@ def hipcc() -> str:
 # does the same: its tiles are a few K steps long, so the epilogue's reads
 # of the accumulators are a large share of its instructions.
 EXTRA_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "attn_packed.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "attn_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "attn_paged.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "gemm_narrow.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}

@@ -1808,6 +1808,8 @@ star_status star_attn_packed_fwd(const star_attn_shape* shape, const void* pack,
   if (!pack || pack_bytes < w.end) return STAR_ERR_WORKSPACE;
   if (!aligned16(pack) || !aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O)) return STAR_ERR_ALIGN;
   if (lse && !aligned4(lse)) return STAR_ERR_ALIGN;
+  // row offsets within a pack are counted in 32 bits of 16 bytes
+  if (static_cast<int64_t>(a.S) * a.H * a.D / 8 > 0xffffffffll) return STAR_ERR_SHAPE;
   const int64_t wgs = pack_main_wgs(a.H, w.max_items);
   if (wgs + pack_clear_wgs(a.S) > 0x7fffff) return STAR_ERR_SHAPE;
   AttnParams p = attn_params(a);
@@ -1819,6 +1821,7 @@ star_status star_attn_packed_fwd(const star_attn_shape* shape, const void* pack,
   p.lse = lse;
   p.pack = pack_view(pack, w);
   p.main_wgs = static_cast<int32_t>(wgs);
+  p.cus = cu_count();
   p.clear_rest = clear_rest;
   return hip_status(launch_attn_packed_fwd(p, stream));
 }
@@ -1826,7 +1829,7 @@ star_status star_attn_packed_fwd(const star_attn_shape* shape, const void* pack,
 size_t star_attn_packed_bwd_workspace_bytes(const star_attn_shape* shape) {
   AttnShape a;
   if (parse_attn(shape, a) != STAR_OK || a.S > kPackMaxTokens) return 0;
-  return align_up(sizeof(float) * a.H * static_cast<size_t>(a.S));
+  return align_up(2 * sizeof(float) * a.H * static_cast<size_t>(a.S));
 }
 
 star_status star_attn_packed_bwd(const star_attn_shape* shape, const void* pack, size_t pack_bytes, const void* dO,
@@ -1847,6 +1850,8 @@ star_status star_attn_packed_bwd(const star_attn_shape* shape, const void* pack,
                         static_cast<const void*>(dV), static_cast<const void*>(ws)})
     if (!aligned16(v)) return STAR_ERR_ALIGN;
   if (!aligned4(lse)) return STAR_ERR_ALIGN;
+  // row offsets within a pack are counted in 32 bits of 16 bytes
+  if (static_cast<int64_t>(a.S) * a.H * a.D / 8 > 0xffffffffll) return STAR_ERR_SHAPE;
   const int64_t q_wgs = pack_main_wgs(a.H, w.max_items), k_wgs = pack_main_wgs(a.Hkv, w.max_items);
   if (q_wgs + pack_clear_wgs(a.S) > 0x7fffff) return STAR_ERR_SHAPE;
   AttnBwdParams p{};
@@ -1856,7 +1861,7 @@ star_status star_attn_packed_bwd(const star_attn_shape* shape, const void* pack,
   p.V = V;
   p.O = O;
   p.lse = lse;
-  p.delta = static_cast<float*>(ws);
+  p.side = static_cast<float*>(ws);
   p.dQ = dQ;
   p.dK = dK;
   p.dV = dV;
@@ -1872,6 +1877,7 @@ star_status star_attn_packed_bwd(const star_attn_shape* shape, const void* pack,
   p.pack = pack_view(pack, w);
   p.q_wgs = static_cast<int32_t>(q_wgs);
   p.k_wgs = static_cast<int32_t>(k_wgs);
+  p.cus = cu_count();
   p.clear_rest = clear_rest;
   return hip_status(launch_attn_packed_bwd(p, stream));
 }

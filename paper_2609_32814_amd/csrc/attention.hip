@@ -78,9 +78,7 @@ template <int DH>
 constexpr int fwd_threads() { return 64 * (kBlockRows / (kQRows * fwd_qtiles<DH>())); }
 
 // M8: groups of 8 features (two groups per 16-feature contraction step).
-// PACKED: sequences of different lengths, one work item of the pack's list
-// per workgroup (see PackView); otherwise B sequences of S positions.
-template <int DH, bool M8, bool PACKED>
+template <int DH, bool M8>
 __global__ __launch_bounds__(fwd_threads<DH>()) void attn_fwd_kernel(const AttnParams p) {
   constexpr int QT = fwd_qtiles<DH>();    // 32-row query tiles per wave
   constexpr int NW = fwd_threads<DH>() / 64;
@@ -94,7 +92,6 @@ __global__ __launch_bounds__(fwd_threads<DH>()) void attn_fwd_kernel(const AttnP
   __shared__ int32_t qpos_s[kBlockRows];
   __shared__ int32_t kpos_s[2][kStepKeys];
   __shared__ int32_t off_s[32 + 1];
-  __shared__ int32_t end_s[PACKED ? 32 : 1];
   __shared__ int32_t nstep_s[32];
   __shared__ uint64_t bits_s[kFwdMaxBlocks / 64];
   // per key type j: the selected chunks in rotated order as a mask, and the
@@ -110,69 +107,52 @@ __global__ __launch_bounds__(fwd_threads<DH>()) void attn_fwd_kernel(const AttnP
   // each XCD takes a contiguous range of (sequence, head) pairs, so the query
   // blocks of one pair run side by side and share its keys and values in that
   // XCD's L2.  Within a pair the latest (longest) query blocks come first.
-  int i = -1, b = 0, h;
-  int32_t q0, nvalid, S = p.S;
-  int64_t seq0 = 0;  // first row of the sequence
-  const int32_t* perm = p.perm;
-  const int32_t* rec = nullptr;
-  if constexpr (PACKED) {
-    if (!pack_matches(p.pack, p.S, p.B, q)) return;
-    if (blockIdx.x >= static_cast<unsigned>(p.main_wgs)) {
-      pack_clear_rows(p.pack, p.S, blockIdx.x - p.main_wgs, p.clear_rest, p.O, p.odtype, p.n_heads * DH, p.lse, p.n_heads);
-      return;
-    }
-    int32_t k;
-    if (!pack_item(p.pack, p.n_heads, h, k)) return;
-    rec = p.pack.recs_q + static_cast<int64_t>(k) * pack_rec_ints(q);
-    seq0 = rec[0];
-    S = rec[1];
-    q0 = rec[2];
-    i = rec[3] & 0xffff;
-    nvalid = rec[3] >> 16;
-    perm = p.pack.perm;
-  } else {
-    const int32_t BH = p.B * p.n_heads;
-    const int64_t n_items = static_cast<int64_t>(BH) * p.items_per_bh;
-    const int64_t per_xcd = (n_items + 7) / 8;
-    const int64_t item = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-    if (item >= n_items) return;
-    const int32_t bh = static_cast<int32_t>(item / p.items_per_bh);
-    int32_t r = static_cast<int32_t>(item % p.items_per_bh);
-    int32_t qb = 0;
-    for (int32_t lvl = 0; i < 0; ++lvl) {
-      bool any = false;
-      for (int t = 0; t < q; ++t) {
-        const int32_t nbt = (p.offsets[t + 1] - p.offsets[t] + kBlockRows - 1) / kBlockRows;
-        if (nbt > lvl) {
-          any = true;
-          if (r == 0) {
-            i = t;
-            qb = nbt - 1 - lvl;
-            break;
-          }
-          --r;
+  const int32_t BH = p.B * p.n_heads;
+  const int64_t n_items = static_cast<int64_t>(BH) * p.items_per_bh;
+  const int64_t per_xcd = (n_items + 7) / 8;
+  const int64_t item = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+  if (item >= n_items) return;
+  const int32_t bh = static_cast<int32_t>(item / p.items_per_bh);
+  int32_t r = static_cast<int32_t>(item % p.items_per_bh);
+  int i = -1;
+  int32_t qb = 0;
+  for (int32_t lvl = 0; i < 0; ++lvl) {
+    bool any = false;
+    for (int t = 0; t < q; ++t) {
+      const int32_t nbt = (p.offsets[t + 1] - p.offsets[t] + kBlockRows - 1) / kBlockRows;
+      if (nbt > lvl) {
+        any = true;
+        if (r == 0) {
+          i = t;
+          qb = nbt - 1 - lvl;
+          break;
         }
+        --r;
       }
-      if (!any) break;
     }
-    if (i < 0) return;  // past the last block (uniform over the workgroup)
-    b = bh / p.n_heads;
-    h = bh % p.n_heads;
-    seq0 = static_cast<int64_t>(b) * p.S;
-    q0 = p.offsets[i] + qb * kBlockRows;
-    nvalid = min(kBlockRows, p.offsets[i + 1] - q0);
+    if (!any) break;
   }
+  if (i < 0) return;  // past the last block (uniform over the workgroup)
+  const int b = bh / p.n_heads, h = bh % p.n_heads;
+  const int32_t q0 = p.offsets[i] + qb * kBlockRows;
+  const int32_t qend = p.offsets[i + 1];
   const int hk = h / (p.n_heads / p.n_kv);
   const int64_t ldq = static_cast<int64_t>(p.n_heads) * DH, ldk = static_cast<int64_t>(p.n_kv) * DH;
-  const uint16_t* Qg = static_cast<const uint16_t*>(p.Q) + seq0 * ldq + h * DH;
-  const uint16_t* Kg = static_cast<const uint16_t*>(p.K) + seq0 * ldk + hk * DH;
-  const uint16_t* Vg = static_cast<const uint16_t*>(p.V) + seq0 * ldk + hk * DH;
+  const uint16_t* Qg = static_cast<const uint16_t*>(p.Q) + static_cast<int64_t>(b) * p.S * ldq + h * DH;
+  const uint16_t* Kg = static_cast<const uint16_t*>(p.K) + static_cast<int64_t>(b) * p.S * ldk + hk * DH;
+  const uint16_t* Vg = static_cast<const uint16_t*>(p.V) + static_cast<int64_t>(b) * p.S * ldk + hk * DH;
 
   // ---- prologue: one round of global loads (the block's query positions,
   // its last query, the first position of every 64-key block of every type,
   // and the key rows of the first two blocks of type 0, the likely first
   // steps), then the step counts.
-  for (int x = threadIdx.x; x < kBlockRows; x += NT) qpos_s[x] = x < nvalid ? perm[q0 + x] : -1;
+  const int32_t nvalid = min(kBlockRows, qend - q0);
+  const int32_t wg_last = p.perm[q0 + nvalid - 1];
+  for (int x = threadIdx.x; x < kBlockRows; x += NT) {
+    const int32_t pos = q0 + x;
+    qpos_s[x] = pos < qend ? p.perm[pos] : -1;
+  }
+  if (threadIdx.x <= q) off_s[threadIdx.x] = p.offsets[threadIdx.x];
   // Groups are taken in the rotated order a' = (a - i) mod q, so that the
   // query's own group i, which every F(i, j) holds, comes first: the first
   // contraction step of every key tile is then always selected.
@@ -185,58 +165,41 @@ __global__ __launch_bounds__(fwd_threads<DH>()) void attn_fwd_kernel(const AttnP
     tab_s[j][0] = csel;
     tab_s[j][1] = __float_as_uint(kLog2e * __builtin_amdgcn_rsqf(static_cast<float>(__popc(fm) * m)));
   }
-  int32_t kp_cur, kp_nxt;
-  if constexpr (PACKED) {
-    // the keys of type j that the block's last query may see
-    if (threadIdx.x < q) {
-      const int32_t off = rec[4 + threadIdx.x], cnt = rec[4 + q + threadIdx.x];
-      off_s[threadIdx.x] = off;
-      end_s[threadIdx.x] = off + cnt;
-      nstep_s[threadIdx.x] = (cnt + kStepKeys - 1) / kStepKeys;
+  const int32_t off0 = p.offsets[0], off1 = p.offsets[1];
+  int32_t kp_cur = off0 + lane < off1 ? p.perm[off0 + lane] : 0x7fffffff;
+  int32_t kp_nxt = off0 + kStepKeys + lane < off1 ? p.perm[off0 + kStepKeys + lane] : 0x7fffffff;
+  // one bit per 64-key block, all types in order: does the block start at
+  // or before the workgroup's last query?
+  int32_t NB = 0;
+  for (int j = 0; j < q; ++j) NB += (p.offsets[j + 1] - p.offsets[j] + kStepKeys - 1) / kStepKeys;
+  for (int32_t x0 = 0; x0 < NB; x0 += NT) {
+    const int32_t x = x0 + threadIdx.x;
+    int32_t first = 0x7fffffff;
+    int32_t base = 0;
+    for (int j = 0; j < q; ++j) {
+      const int32_t oj = p.offsets[j], nb = (p.offsets[j + 1] - oj + kStepKeys - 1) / kStepKeys;
+      if (x >= base && x < base + nb) first = p.perm[oj + kStepKeys * (x - base)];
+      base += nb;
     }
-    const int32_t off0 = rec[4], end0 = off0 + rec[4 + q];
-    kp_cur = off0 + lane < end0 ? perm[off0 + lane] : 0x7fffffff;
-    kp_nxt = off0 + kStepKeys + lane < end0 ? perm[off0 + kStepKeys + lane] : 0x7fffffff;
-    __syncthreads();
-  } else {
-    const int32_t wg_last = p.perm[q0 + nvalid - 1];
-    if (threadIdx.x <= q) off_s[threadIdx.x] = p.offsets[threadIdx.x];
-    const int32_t off0 = p.offsets[0], off1 = p.offsets[1];
-    kp_cur = off0 + lane < off1 ? p.perm[off0 + lane] : 0x7fffffff;
-    kp_nxt = off0 + kStepKeys + lane < off1 ? p.perm[off0 + kStepKeys + lane] : 0x7fffffff;
-    // one bit per 64-key block, all types in order: does the block start at
-    // or before the workgroup's last query?
-    int32_t NB = 0;
-    for (int j = 0; j < q; ++j) NB += (p.offsets[j + 1] - p.offsets[j] + kStepKeys - 1) / kStepKeys;
-    for (int32_t x0 = 0; x0 < NB; x0 += NT) {
-      const int32_t x = x0 + threadIdx.x;
-      int32_t first = 0x7fffffff;
-      int32_t base = 0;
-      for (int j = 0; j < q; ++j) {
-        const int32_t oj = p.offsets[j], nb = (p.offsets[j + 1] - oj + kStepKeys - 1) / kStepKeys;
-        if (x >= base && x < base + nb) first = p.perm[oj + kStepKeys * (x - base)];
-        base += nb;
-      }
-      const uint64_t bal = __ballot(first <= wg_last);
-      if (lane == 0) bits_s[(x0 >> 6) + wave] = bal;
+    const uint64_t bal = __ballot(first <= wg_last);
+    if (lane == 0) bits_s[(x0 >> 6) + wave] = bal;
+  }
+  __syncthreads();
+  // steps of type j: the set bits among its blocks
+  if (threadIdx.x < q) {
+    const int j = threadIdx.x;
+    int32_t base = 0;
+    for (int t = 0; t < j; ++t) base += (off_s[t + 1] - off_s[t] + kStepKeys - 1) / kStepKeys;
+    const int32_t nb = (off_s[j + 1] - off_s[j] + kStepKeys - 1) / kStepKeys;
+    int32_t n = 0;
+    for (int32_t x = base; x < base + nb;) {
+      const int32_t w = x >> 6, lo = x & 63, hi = min(64, lo + (base + nb - x));
+      uint64_t word = bits_s[w] >> lo;
+      if (hi - lo < 64) word &= (1ull << (hi - lo)) - 1ull;
+      n += __popcll(word);
+      x += hi - lo;
     }
-    __syncthreads();
-    // steps of type j: the set bits among its blocks
-    if (threadIdx.x < q) {
-      const int j = threadIdx.x;
-      int32_t base = 0;
-      for (int t = 0; t < j; ++t) base += (off_s[t + 1] - off_s[t] + kStepKeys - 1) / kStepKeys;
-      const int32_t nb = (off_s[j + 1] - off_s[j] + kStepKeys - 1) / kStepKeys;
-      int32_t n = 0;
-      for (int32_t x = base; x < base + nb;) {
-        const int32_t w = x >> 6, lo = x & 63, hi = min(64, lo + (base + nb - x));
-        uint64_t word = bits_s[w] >> lo;
-        if (hi - lo < 64) word &= (1ull << (hi - lo)) - 1ull;
-        n += __popcll(word);
-        x += hi - lo;
-      }
-      nstep_s[j] = n;
-    }
+    nstep_s[j] = n;
   }
   // positions increase along the block: the first and last query of each of
   // the wave's tiles (read through readfirstlane: the compiler then branches
@@ -274,7 +237,6 @@ __global__ __launch_bounds__(fwd_threads<DH>()) void attn_fwd_kernel(const AttnP
   auto nsteps = [&](int j) { return __builtin_amdgcn_readfirstlane(nstep_s[j]); };
   auto tab = [&](int j, int f) { return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(tab_s[j][f])); };
   auto offs = [&](int j) { return __builtin_amdgcn_readfirstlane(off_s[j]); };
-  auto kend = [&](int j) { return __builtin_amdgcn_readfirstlane(PACKED ? end_s[j] : off_s[j + 1]); };
   int32_t T = 0;
   for (int j = 0; j < q; ++j) T += nsteps(j);
 
@@ -297,7 +259,7 @@ __global__ __launch_bounds__(fwd_threads<DH>()) void attn_fwd_kernel(const AttnP
   auto load_kp = [&](const It& it) -> int32_t {
     if (it.j >= q) return 0x7fffffff;
     const int32_t k = offs(it.j) + kStepKeys * it.c + lane;
-    return k < kend(it.j) ? perm[k] : 0x7fffffff;
+    return k < offs(it.j + 1) ? p.perm[k] : 0x7fffffff;
   };
   // global-to-LDS copies of a step's key and value rows (kp: the position of
   // key row `lane`)
@@ -318,7 +280,7 @@ __global__ __launch_bounds__(fwd_threads<DH>()) void attn_fwd_kernel(const AttnP
       const int cp = wave + NW * k;
       const int row = cp * RPC + lane / CPR, c = lane % CPR;
       const int32_t pos = __shfl(kp, row);
-      const bool ok = pos < S;
+      const bool ok = pos < p.S;
       const uint64_t at = (static_cast<uint64_t>(static_cast<uint32_t>(pos)) * row16) << 4;
       const char* kr = reinterpret_cast<const char*>(Kg + 8 * (c ^ key_swz<DH>(row))) + at;
       const char* vr = reinterpret_cast<const char*>(Vg + 8 * (c ^ value_swz<DH>(row))) + at;
@@ -503,7 +465,7 @@ __global__ __launch_bounds__(fwd_threads<DH>()) void attn_fwd_kernel(const AttnP
   for (int u = 0; u < QT; ++u) {
     if (my_qpos[u] < 0) continue;
     const float inv = run_sum[u] > 0.f ? 1.f / run_sum[u] : 0.f;
-    const int64_t o = (seq0 + my_qpos[u]) * ldq + h * DH;
+    const int64_t o = (static_cast<int64_t>(b) * p.S + my_qpos[u]) * ldq + h * DH;
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
@@ -519,8 +481,7 @@ __global__ __launch_bounds__(fwd_threads<DH>()) void attn_fwd_kernel(const AttnP
       }
     if (p.lse && lh == 0) {
       const float l = run_sum[u] > 0.f ? (run_max[u] + __log2f(run_sum[u])) * 0.6931471805599453f : -INFINITY;
-      p.lse[PACKED ? static_cast<int64_t>(h) * p.S + seq0 + my_qpos[u]
-                   : (static_cast<int64_t>(b) * p.n_heads + h) * p.S + my_qpos[u]] = l;
+      p.lse[(static_cast<int64_t>(b) * p.n_heads + h) * p.S + my_qpos[u]] = l;
     }
   }
 }
@@ -740,12 +701,12 @@ __global__ __launch_bounds__(DH) void attn_decode_merge_kernel(const AttnParams 
   store_out(p.O, p.odtype, static_cast<int64_t>(b) * p.n_heads * DH + h * DH + f, v);
 }
 
-template <int DH, bool M8, bool PACKED>
+template <int DH, bool M8>
 hipError_t launch_fwd_dh(const AttnParams& p, unsigned grid, hipStream_t stream) {
   static std::atomic<unsigned long long> set{0};
-  hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(attn_fwd_kernel<DH, M8, PACKED>), set, fwd_smem<DH>());
+  hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(attn_fwd_kernel<DH, M8>), set, fwd_smem<DH>());
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((attn_fwd_kernel<DH, M8, PACKED>), dim3(grid), dim3(fwd_threads<DH>()), fwd_smem<DH>(), stream, p);
+  hipLaunchKernelGGL((attn_fwd_kernel<DH, M8>), dim3(grid), dim3(fwd_threads<DH>()), fwd_smem<DH>(), stream, p);
   return hipGetLastError();
 }
 
@@ -777,25 +738,19 @@ hipError_t launch_decode_dh(const AttnParams& p, hipStream_t stream) {
 
 }  // namespace
 
-template <bool PACKED>
-hipError_t launch_fwd(const AttnParams& p, unsigned grid, hipStream_t stream) {
-  const bool m8 = p.head_dim / p.q == 8;
-  switch (p.head_dim) {
-    case 64: return m8 ? launch_fwd_dh<64, true, PACKED>(p, grid, stream) : launch_fwd_dh<64, false, PACKED>(p, grid, stream);
-    case 128: return m8 ? launch_fwd_dh<128, true, PACKED>(p, grid, stream) : launch_fwd_dh<128, false, PACKED>(p, grid, stream);
-    default: return hipErrorInvalidValue;
-  }
-}
-
 hipError_t launch_attn_fwd(const AttnParams& p, hipStream_t stream) {
   const int64_t items = static_cast<int64_t>(p.B) * p.n_heads * p.items_per_bh;
   const int64_t grid = 8 * ((items + 7) / 8);
   if (items <= 0 || grid > 0x7fffffff) return hipErrorInvalidValue;
-  return launch_fwd<false>(p, static_cast<unsigned>(grid), stream);
-}
-
-hipError_t launch_attn_packed_fwd(const AttnParams& p, hipStream_t stream) {
-  return launch_fwd<true>(p, static_cast<unsigned>(p.main_wgs + pack_clear_wgs(p.S)), stream);
+  switch (p.head_dim) {
+    case 64:
+      return p.head_dim / p.q == 8 ? launch_fwd_dh<64, true>(p, static_cast<unsigned>(grid), stream)
+                                   : launch_fwd_dh<64, false>(p, static_cast<unsigned>(grid), stream);
+    case 128:
+      return p.head_dim / p.q == 8 ? launch_fwd_dh<128, true>(p, static_cast<unsigned>(grid), stream)
+                                   : launch_fwd_dh<128, false>(p, static_cast<unsigned>(grid), stream);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 int32_t attn_decode_chunk(int32_t head_dim, int32_t batch, int32_t n_kv, int32_t head_groups, int32_t S) {

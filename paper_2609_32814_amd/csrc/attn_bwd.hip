@@ -24,172 +24,22 @@
 // P and dS enter their products rounded to bf16 (at most 2^-9 of each term,
 // like the operands themselves); everything else is fp32.
 #include "attn_common.hpp"
+#include "attn_walk.hpp"
 
 namespace starq {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
-constexpr int kStep = 64;  // rows walked per step
-constexpr int32_t kNoPos = 0x7fffffff;
+// -inf for the log-sum-exp of a row that is not there: its probabilities are zero
+__device__ __attribute__((aligned(256))) float g_attn_minus_inf[64] = {-INFINITY};
 
-// Chunk c (16 bytes) of row r of a tile sits at chunk c ^ swz(r).  Two kinds of
-// reads cover all 64 banks: one chunk of 16 rows in 16 lanes (the row operands)
-// and 4 chunks of 4 rows in 32 lanes (the transposing reads).
-template <int DH>
-__device__ __forceinline__ int swz(int r) {
-  return DH == 64 ? 4 * ((r >> 1) & 1) + ((r >> 2) & 3) : 4 * (r & 3) + ((r >> 2) & 3);
-}
-
-template <int DH>
-constexpr int tile_bytes() { return kStep * DH * 2; }
-template <int DH>
-constexpr int smem_bytes() { return 2 * 2 * tile_bytes<DH>(); }  // two stages of two tiles
-
-__device__ __forceinline__ f32x16_t mfma(uint4 a, uint4 b, const f32x16_t& c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
-}
-
-// Per walked type: what its pairs with the block's type select and their scale.
-struct TypeTab {
-  uint32_t rot;    // selected 8-feature cells, the block's own group first
-  uint32_t cells;  // the same in the order of the features
-  float scale;
-};
-
-// The walk of a work item: per type a range of the pack's permutation, in
-// steps of 64 rows; `heads` times over.
-struct Walk {
-  const int32_t* off;    // LDS: first perm index per type
-  const int32_t* cnt;    // LDS: rows per type
-  const int32_t* perm;
-  int q, heads;
-  int hh, j;
-  int32_t c;
-  __device__ __forceinline__ int32_t rows(int t) const { return __builtin_amdgcn_readfirstlane(cnt[t]); }
-  __device__ __forceinline__ void settle() {
-    while (hh < heads && c * kStep >= rows(j)) {
-      c = 0;
-      if (++j == q) {
-        j = 0;
-        ++hh;
-      }
-    }
-  }
-  __device__ __forceinline__ void next() {
-    ++c;
-    settle();
-  }
-  __device__ __forceinline__ bool done() const { return hh >= heads; }
-  // position of row `lane` of the step, or kNoPos
-  __device__ __forceinline__ int32_t pos(int lane) const {
-    if (done()) return kNoPos;
-    const int32_t r = c * kStep + lane;
-    return r < rows(j) ? perm[__builtin_amdgcn_readfirstlane(off[j]) + r] : kNoPos;
-  }
-};
-
-// Copies the rows of one step (lane `row` of kp holds the position of row
-// `row`) of two [T][heads][DH] arrays into a stage.
-template <int DH>
-__device__ __forceinline__ void copy_rows(const uint16_t* A, const uint16_t* B, uint32_t stride16, int32_t kp, char* stage,
-                                          int wave, int lane) {
-  constexpr int CPR = DH / 8, RPC = 64 / CPR;
-#pragma unroll
-  for (int k = 0; k < kStep / RPC / kWaves; ++k) {
-    const int cp = wave + kWaves * k;
-    const int row = cp * RPC + lane / CPR, c = lane % CPR;
-    const int32_t pos = __shfl(kp, row);
-    const bool ok = pos != kNoPos;
-    const uint64_t at = (static_cast<uint64_t>(static_cast<uint32_t>(pos)) * stride16) << 4;
-    const int f = 8 * (c ^ swz<DH>(row));
-    dma16(ok ? reinterpret_cast<const char*>(A + f) + at : reinterpret_cast<const char*>(g_attn_zero), lds_addr(stage + cp * 1024));
-    dma16(ok ? reinterpret_cast<const char*>(B + f) + at : reinterpret_cast<const char*>(g_attn_zero),
-          lds_addr(stage + tile_bytes<DH>() + cp * 1024));
-  }
-}
-
-// The transposed operand of 16 rows from 16 kk on: lane l gets feature
-// 32 c + l % 32 of rows 16 kk + 4 (l / 32) + 0..3 and of the 4 rows 8 behind.
-template <int DH>
-__device__ __forceinline__ uint4 read_transposed(const char* tile, int kk, int c, int lane) {
-  const int g = lane >> 4, rr = (lane & 15) >> 2, qq = lane & 3;
-  const int row = 16 * kk + 4 * (g >> 1) + rr;
-  const int f = 32 * c + 16 * (g & 1) + 4 * qq;
-  const int sub = ((f >> 2) & 1) * 8;
-  const char* a0 = tile + row * DH * 2 + (((f >> 3) ^ swz<DH>(row)) << 4) + sub;
-  const char* a1 = tile + (row + 8) * DH * 2 + (((f >> 3) ^ swz<DH>(row + 8)) << 4) + sub;
-  const uint2 w0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((STARQ_LDS v4i16_t*)(a0)));
-  const uint2 w1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((STARQ_LDS v4i16_t*)(a1)));
-  return make_uint4(w0.x, w0.y, w1.x, w1.y);
-}
-
-// Rows of a transposed product's result: acc[c][4 a + e] is feature
-// 32 c + 8 a + 4 (l / 32) + e of the lane's row.
-template <int DH>
-__device__ __forceinline__ void store_row(void* out, int dtype, int64_t at, const f32x16_t* acc, int lh) {
-#pragma unroll
-  for (int c = 0; c < DH / 32; ++c)
-#pragma unroll
-    for (int a = 0; a < 4; ++a) {
-      const int f = 32 * c + 8 * a + 4 * lh;
-      const float v0 = acc[c][4 * a], v1 = acc[c][4 * a + 1], v2 = acc[c][4 * a + 2], v3 = acc[c][4 * a + 3];
-      if (dtype == 0)
-        *reinterpret_cast<float4*>(static_cast<float*>(out) + at + f) = make_float4(v0, v1, v2, v3);
-      else
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at + f) = make_uint2(pack_bf16(v0, v1), pack_bf16(v2, v3));
-    }
-}
-
-// acc += (rows of `tile`)^T x ops over the features that `cells` selects.
-template <int DH, bool ALL>
-__device__ __forceinline__ void add_transposed(f32x16_t* acc, const char* tile, const uint4* ops, uint32_t cells, int lane) {
-#pragma unroll
-  for (int c = 0; c < DH / 32; ++c) {
-    if (!ALL && !((cells >> (4 * c)) & 15u)) continue;
-    const bool mine = ALL || ((cells >> (4 * c + ((lane & 31) >> 3))) & 1u);
-#pragma unroll
-    for (int kk = 0; kk < kStep / 16; ++kk) {
-      uint4 a = read_transposed<DH>(tile, kk, c, lane);
-      if (!mine) a = make_uint4(0, 0, 0, 0);
-      acc[c] = mfma(a, ops[kk], acc[c]);
-    }
-  }
-}
-
-// What both kernels set up from their record.
-struct ItemLds {
-  int32_t pos[kAttnBlockRows];
-  int32_t off[kAttnMaxQ], cnt[kAttnMaxQ];
-  TypeTab tab[kAttnMaxQ];
-};
-
-__device__ __forceinline__ void setup_item(ItemLds& s, const AttnBwdParams& p, const int32_t* rec, int own) {
-  const int q = p.q, m = p.head_dim / q, cpg = m / 8;
-  const int32_t b0 = rec[2], n = rec[3] >> 16;
-  if (threadIdx.x < kAttnBlockRows) s.pos[threadIdx.x] = static_cast<int32_t>(threadIdx.x) < n ? p.pack.perm[b0 + threadIdx.x] : -1;
-  if (threadIdx.x < static_cast<unsigned>(q)) {
-    const int j = threadIdx.x;
-    s.off[j] = rec[4 + j];
-    s.cnt[j] = rec[4 + q + j];
-    const uint32_t fm = attn_fmask(p.law, q, own, j);  // symmetric in the two types
-    TypeTab t{0, 0, __builtin_amdgcn_rsqf(static_cast<float>(__popc(fm) * m))};
-    for (int a = 0; a < q; ++a) {
-      if ((fm >> a) & 1u) t.cells |= ((1u << cpg) - 1u) << (a * cpg);
-      if ((fm >> ((a + own) % q)) & 1u) t.rot |= ((1u << cpg) - 1u) << (a * cpg);
-    }
-    s.tab[j] = t;
-  }
-}
-
-template <int DH, bool M8>
-__global__ __launch_bounds__(kThreads) void attn_dq_kernel(const AttnBwdParams p) {
-  constexpr int NCH = DH / 32, KS = DH / 16, ROWB = DH * 2, TILE = tile_bytes<DH>();
-  constexpr uint32_t kAll = DH == 64 ? 0xffu : 0xffffu;
-  extern __shared__ __attribute__((aligned(16))) char tiles[];  // [stage][K, V]
-  __shared__ ItemLds it_s;
-  __shared__ int32_t kpos_s[2][kStep];
+// NG groups of four wavefronts take the steps of the walk in turn, each with a
+// ring of its own; their sums meet at the end.
+template <int DH, int NG>
+__global__ __launch_bounds__(NG * kItemThreads, DH == 64 && NG == 1 ? 4 : 2) void attn_dq_kernel(const AttnBwdParams p) {
+  constexpr int NCH = DH / 32, KS = DH / 16, TILE = tile_bytes<DH>(), NC = 2 * copies_per_step<DH>();
+  extern __shared__ __attribute__((aligned(16))) char rings[];  // [group][stage][K, V]
+  __shared__ ItemLds<NG> it_s;
 
   if (!pack_matches(p.pack, p.T, p.n_seq, p.q)) return;
   if (blockIdx.x >= static_cast<unsigned>(p.q_wgs)) {
@@ -199,140 +49,171 @@ __global__ __launch_bounds__(kThreads) void attn_dq_kernel(const AttnBwdParams p
   int h;
   int32_t k;
   if (!pack_item(p.pack, p.n_heads, h, k)) return;
-  const int q = p.q, m = DH / q;
-  const int32_t* rec = p.pack.recs_q + static_cast<int64_t>(k) * pack_rec_ints(q);
+  const int32_t* rec = p.pack.recs_q + static_cast<int64_t>(k) * pack_rec_ints(p.q);
   const int64_t seq0 = rec[0];
-  const int own = rec[3] & 0xffff;
   const int32_t nvalid = rec[3] >> 16;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6) % kItemWaves, g = uniform(threadIdx.x >> 6) / kItemWaves;
   const int lr = lane & 31, lh = lane >> 5;
   const int hk = h / (p.n_heads / p.n_kv);
   const int64_t ldq = static_cast<int64_t>(p.n_heads) * DH, ldk = static_cast<int64_t>(p.n_kv) * DH;
   const uint16_t* Kg = static_cast<const uint16_t*>(p.K) + seq0 * ldk + hk * DH;
   const uint16_t* Vg = static_cast<const uint16_t*>(p.V) + seq0 * ldk + hk * DH;
   const uint32_t ldk16 = static_cast<uint32_t>(ldk >> 3);
-  setup_item(it_s, p, rec, own);
+  const int row0 = wave * 32;
+  const int32_t my = row0 + lr < nvalid ? p.pack.perm[rec[2] + row0 + lr] : -1;
+  setup_item(it_s, rec, p.law, p.q, DH);
   __syncthreads();
 
-  const int row0 = wave * 32;
-  const int32_t tv = min(32, nvalid - row0);
-  const int32_t tfirst = tv > 0 ? __builtin_amdgcn_readfirstlane(it_s.pos[row0]) : kNoPos;
-  const int32_t tlast = tv > 0 ? __builtin_amdgcn_readfirstlane(it_s.pos[row0 + tv - 1]) : -1;
-  const int32_t my = it_s.pos[row0 + lr];
-
-  Walk cur{it_s.off, it_s.cnt, p.pack.perm, q, 1, 0, 0, 0};
-  cur.settle();
-  Walk nxt = cur;
-  nxt.next();
-  int32_t kp = cur.pos(lane), kp_nxt = nxt.pos(lane);
-  copy_rows<DH>(Kg, Vg, ldk16, kp, tiles, wave, lane);
-  if (wave == 0) kpos_s[0][lane] = kp;
-
-  // the wave's rows of Q (own group first) and dO as operands, delta and lse
+  char* tiles = rings + g * ring_bytes<DH>();
+  Walk<NG> wx(&it_s, p.q, 1, g), wp = wx, wc = wx;  // the group's steps h, h + 5, h + 2
+  const int32_t trips = wx.trips();
+  Copies<DH> cp;
+  auto ring = [&](int32_t step) { return it_s.ring[g][step & (kPosSlots - 1)]; };
+  auto ask = [&](int32_t step) {
+    if (wave == 0) ask_positions(wp, p.pack.perm, ring(step), lane);
+    wp.next();
+  };
+  auto copy = [&](int st) {
+    cp.issue(Kg, Vg, ldk16, wc.cells, tiles + st * 2 * TILE, wave, lane);
+    wc.next();
+  };
+  for (int x = 0; x < 4; ++x) ask(x);
+  // the wave's rows of Q and dO as operands, delta and lse (asked for before
+  // the first copies, used behind them)
   uint4 qf[KS], df[KS];
-  int koff[KS], voff[KS];
-  float delta = 0.f, lse2 = 0.f;
+  uint4 of[2 * KS];  // O: 8 values in the first half of each pair, or fp32 in both
   const int64_t qrow = (seq0 + max(my, 0)) * ldq + h * DH;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     const int fr = 16 * ks + 8 * lh;
-    const int fphys = ((fr / m + own) % q) * m + fr % m;
-    koff[ks] = lr * ROWB + (((fphys >> 3) ^ swz<DH>(lr)) << 4);
-    voff[ks] = lr * ROWB + (((fr >> 3) ^ swz<DH>(lr)) << 4);
-    qf[ks] = df[ks] = make_uint4(0, 0, 0, 0);
-    if (my >= 0) {
-      qf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.Q) + qrow + fphys);
-      df[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.dO) + qrow + fr);
-      const uint32_t w[4] = {df[ks].x, df[ks].y, df[ks].z, df[ks].w};
+    qf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.Q) + qrow + fr);
+    df[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.dO) + qrow + fr);
+  }
+  if (p.odtype == 0) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        delta += bf16_to_f32(w[e] & 0xffffu) * load_in(p.O, p.odtype, qrow + fr + 2 * e) +
-                 bf16_to_f32(w[e] >> 16) * load_in(p.O, p.odtype, qrow + fr + 2 * e + 1);
+    for (int ks = 0; ks < KS; ++ks) {
+      const uint4* o = reinterpret_cast<const uint4*>(static_cast<const float*>(p.O) + qrow + 16 * ks + 8 * lh);
+      of[2 * ks] = o[0];
+      of[2 * ks + 1] = o[1];
+    }
+  } else {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      of[2 * ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.O) + qrow + 16 * ks + 8 * lh);
+      of[2 * ks + 1] = make_uint4(0, 0, 0, 0);
+    }
+  }
+  const int64_t at = static_cast<int64_t>(h) * p.T + seq0 + max(my, 0);
+  float lse2 = p.lse[at];
+  // positions ascend along the block: the first and last of the wave's rows
+  const int32_t tv = min(32, nvalid - row0);
+  const int32_t tfirst = tv > 0 ? uniform(my) : kNoPos;
+  const int32_t tlast = tv > 0 ? __builtin_amdgcn_readlane(my, tv - 1) : -1;
+  wait_vm<0>();
+  landed(qf, my >= 0);
+  landed(df, my >= 0);
+  landed(of, my >= 0);
+  landed(lse2);
+  lse2 = my >= 0 ? lse2 * kLog2e : 0.f;
+  __syncthreads();
+  cp.take(ring(0), wave, lane);
+  copy(0);
+  cp.take(ring(1), wave, lane);
+  ask(4);
+  copy(1);
+  cp.take(ring(2), wave, lane);
+  Ends now, then;
+  now.take(ring(0));
+  then.take(ring(1));
+  now = now.settled();
+  then = then.settled();
+
+  float delta = 0.f;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    const uint32_t d[4] = {df[ks].x, df[ks].y, df[ks].z, df[ks].w};
+    const uint4 u = of[2 * ks], v = of[2 * ks + 1];
+    const uint32_t o[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float o0 = p.odtype == 0 ? __uint_as_float(o[2 * e]) : bf16_to_f32(o[e] & 0xffffu);
+      const float o1 = p.odtype == 0 ? __uint_as_float(o[2 * e + 1]) : bf16_to_f32(o[e] >> 16);
+      delta += bf16_to_f32(d[e] & 0xffffu) * o0 + bf16_to_f32(d[e] >> 16) * o1;
     }
   }
   delta = sum_xor32(delta);
-  if (my >= 0) {
-    const int64_t at = static_cast<int64_t>(h) * p.T + seq0 + my;
-    lse2 = p.lse[at] * kLog2e;
-    if (lh == 0) p.delta[at] = delta;
+  if (my >= 0 && lh == 0) {  // for the other launch
+    p.side[at] = -lse2;
+    p.side[at + static_cast<int64_t>(p.n_heads) * p.T] = -delta;
   }
-
   f32x16_t acc[NCH];
 #pragma unroll
   for (int c = 0; c < NCH; ++c) acc[c] = f32x16_t{};
+  TileLane<DH> tl(lane);
 
-  for (int stage = 0; !cur.done(); stage ^= 1) {
-    wait_vm_all();
+  // stage st: the tile of step `step`
+  auto body = [&](int st, int32_t step) {
+    if (wave == 0) wait_vm<NC + 1>();
+    else wait_vm<NC>();
     __syncthreads();
-    Walk nn = nxt;
-    if (!nxt.done()) {
-      nn.next();
-      if (wave == 0) kpos_s[stage ^ 1][lane] = kp_nxt;
-      copy_rows<DH>(Kg, Vg, ldk16, kp_nxt, tiles + (stage ^ 1) * 2 * TILE, wave, lane);
-      kp_nxt = nn.pos(lane);
-    }
-    const char* Kt = tiles + stage * 2 * TILE;
-    const char* Vt = Kt + TILE;
-    const int32_t* kps = kpos_s[stage];
-    const uint32_t rot = __builtin_amdgcn_readfirstlane(it_s.tab[cur.j].rot);
-    const uint32_t cells = __builtin_amdgcn_readfirstlane(it_s.tab[cur.j].cells);
-    const float scale = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(it_s.tab[cur.j].scale)));
-    const float scale2 = scale * kLog2e;
-    const int32_t kf0 = __builtin_amdgcn_readfirstlane(kps[0]);
-    const int32_t kl[2] = {__builtin_amdgcn_readfirstlane(kps[31]), __builtin_amdgcn_readfirstlane(kps[63])};
-    if (kf0 <= tlast) {
-      uint4 pf[4];
+    ask(step + 5);
+    copy((st + 2) % kStages);
+    cp.take(ring(step + 3), wave, lane);
+    Ends after;
+    after.take(ring(step + 2));
+    if (now.first <= tlast) {
+      const char* Kt = tiles + st * 2 * TILE;
+      tl.renew();
+      f32x16_t sc{}, dp{};
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        f32x16_t sc{}, dp{};
+      for (int ks = 0; ks < KS; ++ks) sc = mfma(tl.row(Kt, ks), qf[ks], sc);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          if (ks > 0 && !((rot >> (2 * ks)) & 3u)) continue;
-          uint4 kf = *reinterpret_cast<const uint4*>(Kt + 32 * t * ROWB + koff[ks]);
-          if constexpr (M8) {
-            if (!((rot >> (2 * ks + lh)) & 1u)) kf = make_uint4(0, 0, 0, 0);
-          }
-          sc = mfma(kf, qf[ks], sc);
+      for (int ks = 0; ks < KS; ++ks) dp = mfma(tl.row(Kt + TILE, ks), df[ks], dp);
+      // keys behind a query (rows past a type's end have position kNoPos)
+      if (now.last > tfirst) {
+        const int32_t* kps = ring(step);
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const int4 kq = *reinterpret_cast<const int4*>(kps + 8 * a + 4 * lh);
+          if (kq.x > my) sc[4 * a + 0] = -INFINITY;
+          if (kq.y > my) sc[4 * a + 1] = -INFINITY;
+          if (kq.z > my) sc[4 * a + 2] = -INFINITY;
+          if (kq.w > my) sc[4 * a + 3] = -INFINITY;
         }
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) dp = mfma(*reinterpret_cast<const uint4*>(Vt + 32 * t * ROWB + voff[ks]), df[ks], dp);
-        // keys behind a query (rows past a type's end have position kNoPos)
-        if (kl[t] > tfirst) {
-#pragma unroll
-          for (int a = 0; a < 4; ++a) {
-            const int4 kq = *reinterpret_cast<const int4*>(kps + 32 * t + 8 * a + 4 * lh);
-            if (kq.x > my) sc[4 * a + 0] = -INFINITY, dp[4 * a + 0] = 0.f;
-            if (kq.y > my) sc[4 * a + 1] = -INFINITY, dp[4 * a + 1] = 0.f;
-            if (kq.z > my) sc[4 * a + 2] = -INFINITY, dp[4 * a + 2] = 0.f;
-            if (kq.w > my) sc[4 * a + 3] = -INFINITY, dp[4 * a + 3] = 0.f;
-          }
-        }
-        float ds[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          ds[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale2, -lse2)) * ((dp[e] - delta) * scale);
-#pragma unroll
-        for (int k2 = 0; k2 < 2; ++k2)
-          pf[2 * t + k2] = make_uint4(pack_bf16(ds[8 * k2 + 0], ds[8 * k2 + 1]), pack_bf16(ds[8 * k2 + 2], ds[8 * k2 + 3]),
-                                      pack_bf16(ds[8 * k2 + 4], ds[8 * k2 + 5]), pack_bf16(ds[8 * k2 + 6], ds[8 * k2 + 7]));
       }
-      if (cells == kAll) add_transposed<DH, true>(acc, Kt, pf, cells, lane);
-      else add_transposed<DH, false>(acc, Kt, pf, cells, lane);
+      // dS = scale P (dP - delta): the scale goes into the exponent
+      const float scale2 = wx.scale * kLog2e, base = lse2 - wx.lg;
+      float ds[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) ds[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale2, -base)) * (dp[e] - delta);
+      const uint4 pf[2] = {pack8(ds), pack8(ds + 8)};
+      tl.add_transposed(acc, Kt, pf);
     }
-    cur = nxt;
-    nxt = nn;
+    wx.next();
+    now = then;
+    then = after.settled();
+  };
+
+  for (int32_t n = 0; n < trips; n += 3) {
+    body(0, n);
+    if (n + 1 == trips) break;
+    body(1, n + 1);
+    if (n + 2 == trips) break;
+    body(2, n + 2);
   }
-  if (my >= 0) store_row<DH>(p.dQ, p.gdtype, (seq0 + my) * ldq + h * DH, acc, lh);
+  wait_vm<0>();
+  if constexpr (NG == 2) {
+    if (!join_groups<NCH>(acc, rings, g, wave, lane)) return;
+  }
+  if (my >= 0) store_row<DH>(p.dQ, p.gdtype, qrow, acc, lh);
 }
 
-template <int DH, bool M8>
-__global__ __launch_bounds__(kThreads) void attn_dkv_kernel(const AttnBwdParams p) {
-  constexpr int NCH = DH / 32, KS = DH / 16, ROWB = DH * 2, TILE = tile_bytes<DH>();
-  constexpr uint32_t kAll = DH == 64 ? 0xffu : 0xffffu;
-  extern __shared__ __attribute__((aligned(16))) char tiles[];  // [stage][Q, dO]
-  __shared__ ItemLds it_s;
-  __shared__ int32_t qpos_s[2][kStep];
-  __shared__ float side_s[2][2][kStep];  // [stage][lse (base 2), delta]
+template <int DH, int NG>
+__global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_kernel(const AttnBwdParams p) {
+  constexpr int NCH = DH / 32, KS = DH / 16, TILE = tile_bytes<DH>(), NC = 2 * copies_per_step<DH>();
+  extern __shared__ __attribute__((aligned(16))) char rings[];  // [group][stage][Q, dO]
+  __shared__ ItemLds<NG> it_s;
+  __shared__ __attribute__((aligned(16))) float side_all[NG][kStages][64];  // 32 times -lse (base 2), 32 times -delta
 
   if (!pack_matches(p.pack, p.T, p.n_seq, p.q)) return;
   if (blockIdx.x >= static_cast<unsigned>(p.k_wgs)) {
@@ -343,138 +224,160 @@ __global__ __launch_bounds__(kThreads) void attn_dkv_kernel(const AttnBwdParams 
   int hk;
   int32_t k;
   if (!pack_item(p.pack, p.n_kv, hk, k)) return;
-  const int q = p.q, m = DH / q, rep = p.n_heads / p.n_kv;
-  const int32_t* rec = p.pack.recs_k + static_cast<int64_t>(k) * pack_rec_ints(q);
+  const int rep = p.n_heads / p.n_kv;
+  const int32_t* rec = p.pack.recs_k + static_cast<int64_t>(k) * pack_rec_ints(p.q);
   const int64_t seq0 = rec[0];
-  const int own = rec[3] & 0xffff;
   const int32_t nvalid = rec[3] >> 16;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6) % kItemWaves, g = uniform(threadIdx.x >> 6) / kItemWaves;
   const int lr = lane & 31, lh = lane >> 5;
   const int64_t ldq = static_cast<int64_t>(p.n_heads) * DH, ldk = static_cast<int64_t>(p.n_kv) * DH;
   const uint16_t* Qg = static_cast<const uint16_t*>(p.Q) + seq0 * ldq + hk * rep * DH;
   const uint16_t* Dg = static_cast<const uint16_t*>(p.dO) + seq0 * ldq + hk * rep * DH;
   const uint32_t ldq16 = static_cast<uint32_t>(ldq >> 3);
-  setup_item(it_s, p, rec, own);
+  const int row0 = wave * 32;
+  const int32_t my = row0 + lr < nvalid ? p.pack.perm[rec[2] + row0 + lr] : -1;
+  setup_item(it_s, rec, p.law, p.q, DH);
   __syncthreads();
 
-  const int row0 = wave * 32;
-  const int32_t tv = min(32, nvalid - row0);
-  const int32_t tfirst = tv > 0 ? __builtin_amdgcn_readfirstlane(it_s.pos[row0]) : kNoPos;
-  const int32_t tlast = tv > 0 ? __builtin_amdgcn_readfirstlane(it_s.pos[row0 + tv - 1]) : -1;
-  const int32_t my = it_s.pos[row0 + lr];
-
-  Walk cur{it_s.off, it_s.cnt, p.pack.perm, q, rep, 0, 0, 0};
-  cur.settle();
-  Walk nxt = cur;
-  nxt.next();
-  int32_t qp = cur.pos(lane), qp_nxt = nxt.pos(lane);
-  // wave 0 brings the rows' log-sum-exps, wave 1 their deltas; a row past the
-  // type's end gets +inf, so that its probabilities are zero
-  auto load_side = [&](const Walk& w, int32_t pos) -> float {
-    if (pos == kNoPos) return wave == 0 ? INFINITY : 0.f;
-    const int64_t at = static_cast<int64_t>(hk * rep + w.hh) * p.T + seq0 + pos;
-    return wave == 0 ? p.lse[at] * kLog2e : p.delta[at];
+  char* tiles = rings + g * ring_bytes<DH>();
+  float(*side_s)[64] = side_all[g];
+  Walk<NG> wx(&it_s, p.q, rep, g), wp = wx, wc = wx;  // the group's steps h, h + 5, h + 2
+  const int32_t trips = wx.trips();
+  Copies<DH> cp;
+  int32_t side_pos = kNoPos;
+  auto ring = [&](int32_t step) { return it_s.ring[g][step & (kPosSlots - 1)]; };
+  auto ask = [&](int32_t step) {
+    if (wave == 0) ask_positions(wp, p.pack.perm, ring(step), lane);
+    wp.next();
   };
-  float side = 0.f;
-  copy_rows<DH>(Qg, Dg, ldq16, qp, tiles, wave, lane);
-  if (wave == 0) qpos_s[0][lane] = qp;
-  if (wave < 2) side = load_side(cur, qp);
-
+  auto take = [&](int32_t step) {
+    cp.take(ring(step), wave, lane);
+    side_pos = ring(step)[lr];
+  };
+  // rows, and by wavefront 1 their log-sum-exps and deltas
+  const float* side0 = p.side + (static_cast<int64_t>(lh) * p.n_heads + hk * rep) * p.T + seq0;
+  const float* no_side = lh == 0 ? g_attn_minus_inf : reinterpret_cast<const float*>(cp.zero);
+  auto copy = [&](int st) {
+    if (wave == 1)
+      dma4(side_pos != kNoPos ? side0 + static_cast<int64_t>(wc.hh) * p.T + side_pos : no_side, lds_addr(side_s[st]));
+    cp.issue(Qg + wc.hh * DH, Dg + wc.hh * DH, ldq16, wc.cells, tiles + st * 2 * TILE, wave, lane);
+    wc.next();
+  };
+  for (int x = 0; x < 4; ++x) ask(x);
   uint4 kf[KS], vf[KS];
-  int qoff[KS], doff[KS];
   const int64_t krow = (seq0 + max(my, 0)) * ldk + hk * DH;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     const int fr = 16 * ks + 8 * lh;
-    const int fphys = ((fr / m + own) % q) * m + fr % m;
-    qoff[ks] = lr * ROWB + (((fphys >> 3) ^ swz<DH>(lr)) << 4);
-    doff[ks] = lr * ROWB + (((fr >> 3) ^ swz<DH>(lr)) << 4);
-    kf[ks] = vf[ks] = make_uint4(0, 0, 0, 0);
-    if (my >= 0) {
-      kf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.K) + krow + fphys);
-      vf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.V) + krow + fr);
-    }
+    kf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.K) + krow + fr);
+    vf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.V) + krow + fr);
   }
+  // positions ascend along the block: the first and last of the wave's rows
+  const int32_t tv = min(32, nvalid - row0);
+  const int32_t tfirst = tv > 0 ? uniform(my) : kNoPos;
+  const int32_t tlast = tv > 0 ? __builtin_amdgcn_readlane(my, tv - 1) : -1;
+  wait_vm<0>();
+  landed(kf, my >= 0);
+  landed(vf, my >= 0);
+  __syncthreads();
+  take(0);
+  copy(0);
+  take(1);
+  ask(4);
+  copy(1);
+  take(2);
+  Ends now, then;
+  now.take(ring(0));
+  then.take(ring(1));
+  now = now.settled();
+  then = then.settled();
 
+  // dk is kept in units of the walked type's scale
   f32x16_t dk[NCH], dv[NCH];
 #pragma unroll
   for (int c = 0; c < NCH; ++c) dk[c] = dv[c] = f32x16_t{};
+  float unit = wx.scale;
+  TileLane<DH> tl(lane);
 
-  for (int stage = 0; !cur.done(); stage ^= 1) {
-    wait_vm_all();
-    if (wave < 2) side_s[stage][wave][lane] = side;
+  auto body = [&](int st, int32_t step) {
+    if (wave < 2) wait_vm<NC + 1>();
+    else wait_vm<NC>();
     __syncthreads();
-    Walk nn = nxt;
-    if (!nxt.done()) {
-      nn.next();
-      if (wave == 0) qpos_s[stage ^ 1][lane] = qp_nxt;
-      copy_rows<DH>(Qg + nxt.hh * DH, Dg + nxt.hh * DH, ldq16, qp_nxt, tiles + (stage ^ 1) * 2 * TILE, wave, lane);
-      if (wave < 2) side = load_side(nxt, qp_nxt);
-      qp_nxt = nn.pos(lane);
-    }
-    const char* Qt = tiles + stage * 2 * TILE;
-    const char* Dt = Qt + TILE;
-    const int32_t* qps = qpos_s[stage];
-    const uint32_t rot = __builtin_amdgcn_readfirstlane(it_s.tab[cur.j].rot);
-    const uint32_t cells = __builtin_amdgcn_readfirstlane(it_s.tab[cur.j].cells);
-    const float scale = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(it_s.tab[cur.j].scale)));
-    const float scale2 = scale * kLog2e;
-    const int32_t ql = __builtin_amdgcn_readfirstlane(qps[63]);
-    const int32_t qf0[2] = {__builtin_amdgcn_readfirstlane(qps[0]), __builtin_amdgcn_readfirstlane(qps[32])};
-    if (ql >= tfirst && tv > 0) {
-      uint4 pf[4], sf[4];
+    ask(step + 5);
+    copy((st + 2) % kStages);
+    take(step + 3);
+    Ends after;
+    after.take(ring(step + 2));
+    // positions ascend within a type: a step whose last row lies before the
+    // wave's first key is of no use (kNoPos: the type ends in this step)
+    if (now.last >= tfirst && tv > 0) {
+      const char* Qt = tiles + st * 2 * TILE;
+      tl.renew();
+      if (wx.scale != unit) {
+        const float f = unit * __builtin_amdgcn_rcpf(wx.scale);
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        f32x16_t sc{}, dp{};
+        for (int c = 0; c < NCH; ++c)
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          if (ks > 0 && !((rot >> (2 * ks)) & 3u)) continue;
-          uint4 a = *reinterpret_cast<const uint4*>(Qt + 32 * t * ROWB + qoff[ks]);
-          if constexpr (M8) {
-            if (!((rot >> (2 * ks + lh)) & 1u)) a = make_uint4(0, 0, 0, 0);
-          }
-          sc = mfma(a, kf[ks], sc);
-        }
+          for (int e = 0; e < 16; ++e) dk[c][e] *= f;
+        unit = wx.scale;
+      }
+      f32x16_t sc{}, dp;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) dp = mfma(*reinterpret_cast<const uint4*>(Dt + 32 * t * ROWB + doff[ks]), vf[ks], dp);
-        // queries before a key
-        if (qf0[t] < tlast) {
+      for (int a = 0; a < 4; ++a) {  // dP - delta: the sum starts from -delta
+        const float4 de = *reinterpret_cast<const float4*>(&side_s[st][32 + 8 * a + 4 * lh]);
+        dp[4 * a] = de.x, dp[4 * a + 1] = de.y, dp[4 * a + 2] = de.z, dp[4 * a + 3] = de.w;
+      }
 #pragma unroll
-          for (int a = 0; a < 4; ++a) {
-            const int4 qq = *reinterpret_cast<const int4*>(qps + 32 * t + 8 * a + 4 * lh);
-            if (qq.x < my) sc[4 * a + 0] = -INFINITY;
-            if (qq.y < my) sc[4 * a + 1] = -INFINITY;
-            if (qq.z < my) sc[4 * a + 2] = -INFINITY;
-            if (qq.w < my) sc[4 * a + 3] = -INFINITY;
-          }
-        }
-        float pe[16], ds[16];
+      for (int ks = 0; ks < KS; ++ks) sc = mfma(tl.row(Qt, ks), kf[ks], sc);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) dp = mfma(tl.row(Qt + TILE, ks), vf[ks], dp);
+      if (now.first < tlast) {  // queries before a key
+        const int32_t* qps = ring(step);
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
-          const float4 ls = *reinterpret_cast<const float4*>(&side_s[stage][0][32 * t + 8 * a + 4 * lh]);
-          const float4 de = *reinterpret_cast<const float4*>(&side_s[stage][1][32 * t + 8 * a + 4 * lh]);
-          const float l4[4] = {ls.x, ls.y, ls.z, ls.w}, d4[4] = {de.x, de.y, de.z, de.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            pe[4 * a + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[4 * a + e], scale2, -l4[e]));
-            ds[4 * a + e] = pe[4 * a + e] * ((dp[4 * a + e] - d4[e]) * scale);
-          }
-        }
-#pragma unroll
-        for (int k2 = 0; k2 < 2; ++k2) {
-          const int o = 8 * k2;
-          pf[2 * t + k2] = make_uint4(pack_bf16(pe[o + 0], pe[o + 1]), pack_bf16(pe[o + 2], pe[o + 3]),
-                                      pack_bf16(pe[o + 4], pe[o + 5]), pack_bf16(pe[o + 6], pe[o + 7]));
-          sf[2 * t + k2] = make_uint4(pack_bf16(ds[o + 0], ds[o + 1]), pack_bf16(ds[o + 2], ds[o + 3]),
-                                      pack_bf16(ds[o + 4], ds[o + 5]), pack_bf16(ds[o + 6], ds[o + 7]));
+          const int4 qq = *reinterpret_cast<const int4*>(qps + 8 * a + 4 * lh);
+          if (qq.x < my) sc[4 * a + 0] = -INFINITY;
+          if (qq.y < my) sc[4 * a + 1] = -INFINITY;
+          if (qq.z < my) sc[4 * a + 2] = -INFINITY;
+          if (qq.w < my) sc[4 * a + 3] = -INFINITY;
         }
       }
-      add_transposed<DH, true>(dv, Dt, pf, kAll, lane);
-      if (cells == kAll) add_transposed<DH, true>(dk, Qt, sf, cells, lane);
-      else add_transposed<DH, false>(dk, Qt, sf, cells, lane);
+      const float scale2 = wx.scale * kLog2e;
+      float pe[16], ds[16];
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const float4 ls = *reinterpret_cast<const float4*>(&side_s[st][8 * a + 4 * lh]);
+        const float l4[4] = {ls.x, ls.y, ls.z, ls.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          pe[4 * a + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[4 * a + e], scale2, l4[e]));
+          ds[4 * a + e] = pe[4 * a + e] * dp[4 * a + e];
+        }
+      }
+      const uint4 pf[2] = {pack8(pe), pack8(pe + 8)}, sf[2] = {pack8(ds), pack8(ds + 8)};
+      tl.add_transposed(dv, Qt + TILE, pf);
+      tl.add_transposed(dk, Qt, sf);
     }
-    cur = nxt;
-    nxt = nn;
+    wx.next();
+    now = then;
+    then = after.settled();
+  };
+
+  for (int32_t n = 0; n < trips; n += 3) {
+    body(0, n);
+    if (n + 1 == trips) break;
+    body(1, n + 1);
+    if (n + 2 == trips) break;
+    body(2, n + 2);
+  }
+  wait_vm<0>();
+#pragma unroll
+  for (int c = 0; c < NCH; ++c)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dk[c][e] *= unit;
+  if constexpr (NG == 2) {
+    join_groups<NCH>(dk, rings, g, wave, lane);
+    if (!join_groups<NCH>(dv, rings, g, wave, lane)) return;
   }
   if (my >= 0) {
     store_row<DH>(p.dK, p.gdtype, krow, dk, lh);
@@ -482,29 +385,39 @@ __global__ __launch_bounds__(kThreads) void attn_dkv_kernel(const AttnBwdParams 
   }
 }
 
-template <int DH, bool M8>
-hipError_t launch_dh(const AttnBwdParams& p, hipStream_t stream) {
+template <int DH, int NQ, int NK>
+hipError_t launch_groups(const AttnBwdParams& p, hipStream_t stream) {
   static std::atomic<unsigned long long> set_q{0}, set_k{0};
-  constexpr int smem = smem_bytes<DH>();
-  hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(attn_dq_kernel<DH, M8>), set_q, smem);
+  const auto dq = attn_dq_kernel<DH, NQ>;
+  const auto dkv = attn_dkv_kernel<DH, NK>;
+  constexpr int smem = ring_bytes<DH>();
+  hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(dq), set_q, NQ * smem);
   if (e != hipSuccess) return e;
-  e = ensure_lds_limit(reinterpret_cast<const void*>(attn_dkv_kernel<DH, M8>), set_k, smem);
+  e = ensure_lds_limit(reinterpret_cast<const void*>(dkv), set_k, NK * smem);
   if (e != hipSuccess) return e;
   const unsigned clear = static_cast<unsigned>(pack_clear_wgs(p.T));
-  hipLaunchKernelGGL((attn_dq_kernel<DH, M8>), dim3(p.q_wgs + clear), dim3(kThreads), smem, stream, p);
+  hipLaunchKernelGGL(dq, dim3(p.q_wgs + clear), dim3(NQ * kItemThreads), NQ * smem, stream, p);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((attn_dkv_kernel<DH, M8>), dim3(p.k_wgs + clear), dim3(kThreads), smem, stream, p);
+  hipLaunchKernelGGL(dkv, dim3(p.k_wgs + clear), dim3(NK * kItemThreads), NK * smem, stream, p);
   return hipGetLastError();
+}
+
+template <int DH, int NK>
+hipError_t launch_dh(const AttnBwdParams& p, hipStream_t stream) {
+  const bool few_q = pack_few(p.q_wgs, p.cus), few_k = NK == 2 || pack_few(p.k_wgs, p.cus);
+  if (few_q) return few_k ? launch_groups<DH, 2, 2>(p, stream) : launch_groups<DH, 2, NK>(p, stream);
+  return few_k ? launch_groups<DH, 1, 2>(p, stream) : launch_groups<DH, 1, NK>(p, stream);
 }
 
 }  // namespace
 
 hipError_t launch_attn_packed_bwd(const AttnBwdParams& p, hipStream_t stream) {
-  const bool m8 = p.head_dim / p.q == 8;
   switch (p.head_dim) {
-    case 64: return m8 ? launch_dh<64, true>(p, stream) : launch_dh<64, false>(p, stream);
-    case 128: return m8 ? launch_dh<128, true>(p, stream) : launch_dh<128, false>(p, stream);
+    // (head width 128: the registers hold two wavefronts of dK and dV a SIMD
+    // either way, and with two groups the longest walk is half as long)
+    case 64: return launch_dh<64, 1>(p, stream);
+    case 128: return launch_dh<128, 2>(p, stream);
     default: return hipErrorInvalidValue;
   }
 }

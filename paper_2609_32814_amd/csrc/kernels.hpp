@@ -318,6 +318,7 @@ struct AttnParams {
   // packed: B sequences, S rows in all
   PackView pack;
   int32_t main_wgs;    // workgroups of the work items; the others clear rows
+  int32_t cus;         // compute units of the device
   int32_t clear_rest;  // rows outside every sequence are written as zeros
   // decode: S is the cache capacity; one query row per sequence
   const int32_t* pos_type;   // [S]
@@ -342,7 +343,7 @@ struct AttnBwdParams {
   const void* V;
   const void* O;
   const float* lse;  // [n_heads][T]
-  float* delta;      // [n_heads][T]: <dO, O> of every row
+  float* side;       // [2][n_heads][T]: minus the log-sum-exp (base 2), minus <dO, O> of every row
   void* dQ;
   void* dK;
   void* dV;
@@ -350,6 +351,7 @@ struct AttnBwdParams {
   int32_t T, n_seq, n_heads, n_kv, head_dim, q, law;
   PackView pack;
   int32_t q_wgs, k_wgs;  // workgroups of the work items of either launch
+  int32_t cus;
   int32_t clear_rest;
 };
 hipError_t launch_attn_packed_bwd(const AttnBwdParams& p, hipStream_t stream);
@@ -372,6 +374,9 @@ inline int64_t pack_main_wgs(int32_t heads, int32_t max_items) {
   return int64_t{8} * g.per_xcd * ((max_items + g.cuts - 1) / g.cuts);
 }
 constexpr int32_t kPackClearRows = 256;
+// Few work items (an upper bound of them) for the chip: two groups of
+// wavefronts then share a walk.
+inline bool pack_few(int64_t main_wgs, int32_t cus) { return main_wgs <= 2 * static_cast<int64_t>(cus); }
 inline int64_t pack_clear_wgs(int32_t T) { return (T + kPackClearRows - 1) / kPackClearRows; }
 
 // Keys per decode split for a shape (a multiple of the 4 keys per team of
