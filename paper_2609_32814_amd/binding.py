@@ -912,12 +912,13 @@ def star_attn_packed_fwd(shape: AttnShape, pack: torch.Tensor, Q: torch.Tensor, 
     _need(V, "V", (T, Hkv, D), _BF16, dev)
     _need(pack, "pack", (pack.numel(),), (torch.uint8,), dev)
     clear = O is None
-    if O is None:
+    if clear:
         O = torch.empty((T, H, D), dtype=out_dtype, device=dev)
     _need(O, "O", (T, H, D), _FLOATS, dev)
-    if lse is None and want_lse:
+    if lse is not None:
+        _need(lse, "lse", (H, T), _F32, dev)
+    elif want_lse:
         lse = torch.empty((H, T), dtype=torch.float32, device=dev)
-    _opt(lse, "lse", (H, T), _F32, dev)
     _gpu(dev)
     _check(LIB.star_attn_packed_fwd(shape.ref, _ptr(pack), pack.numel(), _ptr(Q), _ptr(K), _ptr(V),
                                     DTYPES[torch.bfloat16], _ptr(O), _dt(O), _ptr(lse), int(clear), _stream(dev)),
@@ -1044,11 +1045,12 @@ def star_kv_read(pages: KVPages, cu_seqlens: torch.Tensor, cache_len: torch.Tens
     if (K is None) != (V is None):
         raise ValueError("give both of K and V, or none")
     clear = K is None
+    shape = (int(T), pages.n_kv_heads, pages.head_dim)
     if clear:
-        K, V = (torch.empty((int(T), pages.n_kv_heads, pages.head_dim), dtype=torch.bfloat16, device=dev)
-                for _ in range(2))
-    _need(K, "K", (int(T), pages.n_kv_heads, pages.head_dim), _BF16, dev)
-    _need(V, "V", (int(T), pages.n_kv_heads, pages.head_dim), _BF16, dev)
+        K, V = torch.empty(shape, dtype=torch.bfloat16, device=dev), torch.empty(shape, dtype=torch.bfloat16, device=dev)
+    else:
+        _need(K, "K", shape, _BF16, dev)
+        _need(V, "V", shape, _BF16, dev)
     _check(LIB.star_kv_read(pages.ref, _ptr(cu_seqlens), _ptr(cache_len), int(T), _ptr(K), _ptr(V),
                             DTYPES[torch.bfloat16], int(clear), _stream(dev)), "star_kv_read")
     return K, V

@@ -1752,8 +1752,8 @@ star_status check_pages(const KvPages& kv) {
 star_status check_rows(const KvPages& kv, int64_t T, const int32_t* cu, const int32_t* cache_len, const void* K,
                        const void* V, star_dtype dt) {
   if (dt != STAR_BF16) return STAR_ERR_DTYPE;
-  // a thread per 8 elements, in one grid
-  if (T < 0 || T > 0x7fffffff || T * kv.n_kv > (int64_t{1} << 34)) return STAR_ERR_SHAPE;
+  if (T < 0 || T > 0x7fffff00) return STAR_ERR_SHAPE;
+  if (kv.n_kv > (1 << 20)) return STAR_ERR_SHAPE;  // 16 n_kv rows of a workgroup are counted in 32 bits
   if (T == 0) return STAR_OK;
   if (!cu || !cache_len || !K || !V) return STAR_ERR_ARG;
   if (!aligned4(cu) || !aligned4(cache_len) || !aligned16(K) || !aligned16(V)) return STAR_ERR_ALIGN;
@@ -1761,14 +1761,18 @@ star_status check_rows(const KvPages& kv, int64_t T, const int32_t* cu, const in
 }
 
 struct PagedWs {
-  int32_t wgs = 0;
+  int32_t waves = 0;
   size_t part_o = 0, part_ml = 0, end = 0;
 };
 PagedWs paged_layout(const AttnShape& a) {
   PagedWs w;
   const int32_t rep = a.H / a.Hkv;
-  w.wgs = paged_workgroups(cu_count());
-  const size_t slots = (static_cast<size_t>(a.B) * a.Hkv * paged_groups(rep) + w.wgs) * paged_slice(rep);
+  w.waves = paged_waves(cu_count());
+  if (!paged_splits(a.S)) {
+    w.end = kAlign;
+    return w;
+  }
+  const size_t slots = (static_cast<size_t>(a.B) * a.Hkv * paged_groups(rep) + w.waves) * paged_slice(rep);
   w.part_o = 0;
   w.part_ml = align_up(sizeof(float) * slots * a.D);
   w.end = align_up(w.part_ml + sizeof(float) * 2 * slots);
@@ -1940,7 +1944,8 @@ star_status star_attn_decode_paged(const star_attn_shape* shape, const star_kv_p
   p.q = a.q;
   p.law = a.law;
   p.groups = paged_groups(a.H / a.Hkv);
-  p.wgs = w.wgs;
+  p.waves = w.waves;
+  p.split = paged_splits(a.S);
   p.part_o = at<float>(ws, w.part_o);
   p.part_ml = at<float>(ws, w.part_ml);
   return hip_status(launch_attn_decode_paged(p, stream));

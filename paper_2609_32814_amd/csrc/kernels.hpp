@@ -418,14 +418,16 @@ struct AttnPagedParams {
   int32_t cap;               // max_pages pages
   int32_t n_heads, q, law;
   int32_t groups;            // slices of kPagedHeads query heads per key/value head
-  int32_t wgs;               // workgroups that share the tiles
-  float* part_o;             // [wgs + B n_kv groups][heads of a slice][head_dim]
+  int32_t waves;             // wavefronts that share the tiles
+  int32_t split;             // 0: a workgroup takes a whole pair (and there are no pieces)
+  float* part_o;             // [waves + B n_kv groups][heads of a slice][head_dim]
   float* part_ml;            // [...][heads of a slice][2]: maximum (base 2), sum
 };
 constexpr int kPagedHeads = 16;  // query heads per workgroup (the columns of a 16 x 16 product)
 STARQ_HD inline int32_t paged_groups(int32_t rep) { return (rep + kPagedHeads - 1) / kPagedHeads; }
 STARQ_HD inline int32_t paged_slice(int32_t rep) { return rep < kPagedHeads ? rep : kPagedHeads; }
-int32_t paged_workgroups(int cus);
+int32_t paged_waves(int cus);
+bool paged_splits(int32_t cap);  // whether a pair's keys may be split (a second launch then joins them)
 hipError_t launch_attn_decode_paged(const AttnPagedParams& p, hipStream_t stream);
 
 // The static workspace of star_decode_noalloc (scratch.hip): its size, and

@@ -9,9 +9,11 @@
 // loses nothing by it, int8 at most one bit of its seven.  A row that holds a
 // NaN or an infinity is kept as scale byte 255 and reads back as NaN.
 //
-// head_dim / 8 lanes take a row, 16 bytes of bf16 each; the row's largest
-// magnitude is joined by lane exchanges.  Both kernels are bound by memory:
-// every row is read once and written once.
+// A workgroup takes TG tokens: it looks each one's place up once, then goes
+// through the rows of all their heads, 16 bytes of a page row to a lane, the
+// rows of one head's tokens side by side (they are neighbours in the page).  A
+// row's largest magnitude is joined by lane exchanges.  Both kernels are bound
+// by memory: every row is read once and written once.
 #include "attn_common.hpp"
 #include "kv_common.hpp"
 
@@ -38,116 +40,147 @@ __device__ __forceinline__ int64_t find_row(const KvPages& kv, const int32_t* cu
   return ((static_cast<int64_t>(page) * kv.n_kv) << kv.page_shift) + (pos & ((1 << kv.page_shift) - 1));
 }
 
-// 8 elements of a row to 8 bytes; LANES lanes hold the row.  Returns the scale byte.
+// Elements of a row that a lane holds: 16 bytes of the page.
+template <int TYPE>
+constexpr int lane_elems() { return TYPE == kKvBf16 ? 8 : 16; }
+
+// 16 elements of a row (in[0], in[1]) to 16 bytes; LANES lanes hold the row.
+// Returns the scale byte.
 template <int TYPE, int LANES>
-__device__ __forceinline__ int quantise(const uint4& in, uint2& out) {
-  const uint32_t w[4] = {in.x, in.y, in.z, in.w};
+__device__ __forceinline__ int quantise(const uint4* in, uint4& out) {
+  const uint32_t w[8] = {in[0].x, in[0].y, in[0].z, in[0].w, in[1].x, in[1].y, in[1].z, in[1].w};
   uint32_t top = 0;  // largest magnitude as bits: their order is that of the values, NaN above all
 #pragma unroll
-  for (int e = 0; e < 4; ++e) top = max(top, max((w[e] << 16) & 0x7fff0000u, w[e] & 0x7fff0000u));
+  for (int e = 0; e < 8; ++e) top = max(top, max((w[e] << 16) & 0x7fff0000u, w[e] & 0x7fff0000u));
 #pragma unroll
   for (int d = LANES / 2; d > 0; d >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), d, LANES)));
-  out = make_uint2(0, 0);
+  out = make_uint4(0, 0, 0, 0);
   if (top >= 0x7f800000u) return 255;
   // top = 1.f 2^k against 1.75 2^8 or 1.984375 2^6
   constexpr uint32_t kFrac = TYPE == kKvE4m3 ? 0x600000u : 0x7e0000u;
   constexpr int kExp = TYPE == kKvE4m3 ? 8 : 6;
   const int scale = max(1, static_cast<int>(top >> 23) - kExp + ((top & 0x7fffffu) > kFrac ? 1 : 0));
   const float inv = __uint_as_float(static_cast<uint32_t>(254 - scale) << 23);
-  float y[8];
+  uint32_t v[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    y[2 * e] = __uint_as_float(w[e] << 16) * inv;
-    y[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u) * inv;
+  for (int x = 0; x < 4; ++x) {
+    const float y0 = __uint_as_float(w[2 * x] << 16) * inv, y1 = __uint_as_float(w[2 * x] & 0xffff0000u) * inv;
+    const float y2 = __uint_as_float(w[2 * x + 1] << 16) * inv, y3 = __uint_as_float(w[2 * x + 1] & 0xffff0000u) * inv;
+    if constexpr (TYPE == kKvE4m3) {
+      v[x] = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(y2, y3, __builtin_amdgcn_cvt_pk_fp8_f32(y0, y1, 0, false), true));
+    } else {
+      auto byte = [](float y) { return static_cast<uint32_t>(static_cast<int>(__builtin_rintf(y))) & 0xffu; };
+      v[x] = byte(y0) | byte(y1) << 8 | byte(y2) << 16 | byte(y3) << 24;
+    }
   }
-  if constexpr (TYPE == kKvE4m3) {
-    int a = 0, b = 0;
-    a = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], a, false);
-    a = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], a, true);
-    b = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], b, false);
-    b = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], b, true);
-    out = make_uint2(a, b);
-  } else {
-    uint32_t v[2] = {0, 0};
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      v[e / 4] |= (static_cast<uint32_t>(static_cast<int>(__builtin_rintf(y[e]))) & 0xffu) << (8 * (e % 4));
-    out = make_uint2(v[0], v[1]);
-  }
+  out = make_uint4(v[0], v[1], v[2], v[3]);
   return scale;
 }
 
+// The places of the workgroup's TG tokens, then `each(row, token, head, c)` for
+// every row of them: its place (see find_row), and which of its lanes this is.
+template <int DH, int TYPE, int TG, class Each>
+__device__ __forceinline__ void for_rows(const KvPages& kv, const int32_t* cu, const int32_t* cache_len, int32_t T, Each each) {
+  constexpr int LANES = DH / lane_elems<TYPE>(), RP = kThreads / LANES;
+  __shared__ int64_t place[TG];
+  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * TG;
+  if (threadIdx.x < TG) place[threadIdx.x] = t0 + threadIdx.x < T ? find_row(kv, cu, cache_len, static_cast<int32_t>(t0 + threadIdx.x)) : -3;
+  __syncthreads();
+  const int c = threadIdx.x % LANES;
+#pragma unroll 4
+  for (int32_t r = threadIdx.x / LANES; r < TG * kv.n_kv; r += RP) {
+    const int32_t head = r / TG;
+    int64_t row = place[r % TG];
+    if (row >= 0) row += static_cast<int64_t>(head) << kv.page_shift;
+    each(row, t0 + r % TG, head, c);
+  }
+}
+
 // blockIdx.y 0: keys, 1: values
-template <int DH, int TYPE>
+template <int DH, int TYPE, int TG>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(const KvPages kv, const int32_t* cu, const int32_t* cache_len,
                                                              int32_t T, const uint16_t* K, const uint16_t* V) {
-  constexpr int LANES = DH / 8;
-  const int64_t r = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / LANES;  // token n_kv + head
-  const int c = threadIdx.x % LANES;
-  if (r >= static_cast<int64_t>(T) * kv.n_kv) return;  // (a row's lanes together)
-  const int32_t t = static_cast<int32_t>(r / kv.n_kv), head = static_cast<int32_t>(r % kv.n_kv);
-  const uint4 in = *reinterpret_cast<const uint4*>((blockIdx.y ? V : K) + r * DH + 8 * c);
-  int64_t row = find_row(kv, cu, cache_len, t);
-  if (row < 0) return;
-  row += static_cast<int64_t>(head) << kv.page_shift;
-  void* pages = blockIdx.y ? kv.V : kv.K;
-  if constexpr (TYPE == kKvBf16) {
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(pages) + row * DH + 8 * c) = in;
-  } else {
-    uint2 out;
-    const int scale = quantise<TYPE, LANES>(in, out);
-    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(pages) + row * DH + 8 * c) = out;
-    if (c == 0) (blockIdx.y ? kv.v_scale : kv.k_scale)[row] = static_cast<uint8_t>(scale);
-  }
+  constexpr int LE = lane_elems<TYPE>();
+  const uint16_t* src = blockIdx.y ? V : K;
+  uint4* pages = static_cast<uint4*>(blockIdx.y ? kv.V : kv.K);
+  uint8_t* scales = blockIdx.y ? kv.v_scale : kv.k_scale;
+  for_rows<DH, TYPE, TG>(kv, cu, cache_len, T, [&](int64_t row, int64_t t, int32_t head, int c) {
+    if (row < 0) return;  // (a row's lanes together)
+    const uint4* in = reinterpret_cast<const uint4*>(src + (t * kv.n_kv + head) * DH + LE * c);
+    uint4* to = pages + row * (DH / LE) + c;
+    if constexpr (TYPE == kKvBf16) {
+      *to = *in;
+    } else {
+      const uint4 w[2] = {in[0], in[1]};
+      uint4 out;
+      const int scale = quantise<TYPE, DH / LE>(w, out);
+      *to = out;
+      if (c == 0) scales[row] = static_cast<uint8_t>(scale);
+    }
+  });
 }
 
-template <int DH, int TYPE>
+template <int DH, int TYPE, int TG>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(const KvPages kv, const int32_t* cu, const int32_t* cache_len,
                                                            int32_t T, uint16_t* K, uint16_t* V, int32_t clear_rest) {
-  constexpr int LANES = DH / 8;
-  const int64_t r = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / LANES;
-  const int c = threadIdx.x % LANES;
-  if (r >= static_cast<int64_t>(T) * kv.n_kv) return;
-  const int32_t t = static_cast<int32_t>(r / kv.n_kv), head = static_cast<int32_t>(r % kv.n_kv);
-  int64_t row = find_row(kv, cu, cache_len, t);
-  if (row == -2 && !clear_rest) return;
-  uint4 out = make_uint4(0, 0, 0, 0);
-  if (row >= 0) {
-    row += static_cast<int64_t>(head) << kv.page_shift;
-    const void* pages = blockIdx.y ? kv.V : kv.K;
+  constexpr int LE = lane_elems<TYPE>();
+  uint16_t* dst = blockIdx.y ? V : K;
+  const uint4* pages = static_cast<const uint4*>(blockIdx.y ? kv.V : kv.K);
+  const uint8_t* scales = blockIdx.y ? kv.v_scale : kv.k_scale;
+  for_rows<DH, TYPE, TG>(kv, cu, cache_len, T, [&](int64_t row, int64_t t, int32_t head, int c) {
+    if (row == -3 || (row == -2 && !clear_rest)) return;
+    uint4* to = reinterpret_cast<uint4*>(dst + (t * kv.n_kv + head) * DH + LE * c);
+    uint4 in = make_uint4(0, 0, 0, 0);
+    if (row >= 0) in = pages[row * (DH / LE) + c];
     if constexpr (TYPE == kKvBf16) {
-      out = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(pages) + row * DH + 8 * c);
+      *to = in;
     } else {
-      const uint2 in = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pages) + row * DH + 8 * c);
-      const float s = kv_scale((blockIdx.y ? kv.v_scale : kv.k_scale)[row]);
-      float y[8];
-      kv_unpack4<TYPE>(in.x, y);
-      kv_unpack4<TYPE>(in.y, y + 4);
-      out = make_uint4(pack_bf16(y[0] * s, y[1] * s), pack_bf16(y[2] * s, y[3] * s), pack_bf16(y[4] * s, y[5] * s),
-                       pack_bf16(y[6] * s, y[7] * s));
+      const float s = row >= 0 ? kv_scale(scales[row], 0) : 0.f;
+      const uint32_t w[4] = {in.x, in.y, in.z, in.w};
+      uint32_t o[8];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        float y[4];
+        kv_unpack4<TYPE>(w[x], y);
+        o[2 * x] = pack_bf16(y[0] * s, y[1] * s);
+        o[2 * x + 1] = pack_bf16(y[2] * s, y[3] * s);
+      }
+      to[0] = make_uint4(o[0], o[1], o[2], o[3]);
+      to[1] = make_uint4(o[4], o[5], o[6], o[7]);
     }
-  }
-  *reinterpret_cast<uint4*>((blockIdx.y ? V : K) + r * DH + 8 * c) = out;
+  });
 }
 
-unsigned rows_grid(const KvPages& kv, int32_t T) {
-  const int64_t lanes = static_cast<int64_t>(T) * kv.n_kv * (kv.head_dim / 8);
-  return static_cast<unsigned>((lanes + kThreads - 1) / kThreads);
-}
+// 16 tokens a workgroup; 4 where that would leave CUs without one (64 tokens of
+// 12 heads of 64 to int8 and back: FILL)
+constexpr int kMany = 16, kFew = 4;
+bool few_tokens(int32_t T) { return T < 256 * kMany; }
 
+template <int DH, int TYPE, int TG>
+hipError_t append_tg(const KvPages& kv, const int32_t* cu, const int32_t* len, int32_t T, const void* K, const void* V,
+                     hipStream_t stream) {
+  hipLaunchKernelGGL((kv_append_kernel<DH, TYPE, TG>), dim3((T + TG - 1) / TG, 2), dim3(kThreads), 0, stream, kv, cu, len, T,
+                     static_cast<const uint16_t*>(K), static_cast<const uint16_t*>(V));
+  return hipGetLastError();
+}
 template <int DH, int TYPE>
 hipError_t append(const KvPages& kv, const int32_t* cu, const int32_t* len, int32_t T, const void* K, const void* V,
                   hipStream_t stream) {
-  hipLaunchKernelGGL((kv_append_kernel<DH, TYPE>), dim3(rows_grid(kv, T), 2), dim3(kThreads), 0, stream, kv, cu, len, T,
-                     static_cast<const uint16_t*>(K), static_cast<const uint16_t*>(V));
+  return few_tokens(T) ? append_tg<DH, TYPE, kFew>(kv, cu, len, T, K, V, stream)
+                       : append_tg<DH, TYPE, kMany>(kv, cu, len, T, K, V, stream);
+}
+template <int DH, int TYPE, int TG>
+hipError_t read_tg(const KvPages& kv, const int32_t* cu, const int32_t* len, int32_t T, void* K, void* V, int32_t clear_rest,
+                   hipStream_t stream) {
+  hipLaunchKernelGGL((kv_read_kernel<DH, TYPE, TG>), dim3((T + TG - 1) / TG, 2), dim3(kThreads), 0, stream, kv, cu, len, T,
+                     static_cast<uint16_t*>(K), static_cast<uint16_t*>(V), clear_rest);
   return hipGetLastError();
 }
 template <int DH, int TYPE>
 hipError_t read(const KvPages& kv, const int32_t* cu, const int32_t* len, int32_t T, void* K, void* V, int32_t clear_rest,
                 hipStream_t stream) {
-  hipLaunchKernelGGL((kv_read_kernel<DH, TYPE>), dim3(rows_grid(kv, T), 2), dim3(kThreads), 0, stream, kv, cu, len, T,
-                     static_cast<uint16_t*>(K), static_cast<uint16_t*>(V), clear_rest);
-  return hipGetLastError();
+  return few_tokens(T) ? read_tg<DH, TYPE, kFew>(kv, cu, len, T, K, V, clear_rest, stream)
+                       : read_tg<DH, TYPE, kMany>(kv, cu, len, T, K, V, clear_rest, stream);
 }
 
 }  // namespace

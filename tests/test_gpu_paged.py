@@ -276,6 +276,30 @@ def test_values_that_are_masked_may_be_anything(P):
         assert torch.equal(O, want) and bool(torch.isfinite(O).all())
 
 
+@pytest.mark.parametrize("kv", ["e4m3", "int8"])
+def test_scales_of_masked_rows_may_be_anything(P, kv):
+    """Rows that are not finite, and places that hold no row, with scale byte
+    255: a position of no type, positions behind the end of the sequence."""
+    c = Cache(P, kv, 1, 64, 16, 1, 4)
+    K, V = rnd((40, 1, 64), 1), rnd((40, 1, 64), 2)
+    t = ref.cyclic(64, 4)
+    t[5] = 9
+    out = []
+    for poison in (False, True):
+        Kp, Vp = K.clone(), V.clone()
+        if poison:
+            Kp[5], Vp[5] = torch.nan, torch.inf
+            c.ks.fill_(255)
+            c.vs.fill_(255)
+        P.star_kv_append(c.pages, i32([0, 40]), i32([40]), Kp.to(DEV), Vp.to(DEV))
+        out.append(P.star_attn_decode_paged(P.AttnShape(1, 64, 2, 1, 64, 4), c.pages, t.to(DEV), i32([35]), rnd((1, 2, 64), 3).to(DEV)))
+    assert torch.equal(out[0], out[1]) and bool(torch.isfinite(out[0]).all())
+    # a row that counts and is not finite: NaN for the heads that see it
+    t[5] = 1
+    assert bool(torch.isnan(P.star_attn_decode_paged(P.AttnShape(1, 64, 2, 1, 64, 4), c.pages, t.to(DEV), i32([35]),
+                                                     rnd((1, 2, 64), 3).to(DEV))).all())
+
+
 def test_offsets_past_32_bits(P):
     """A cache of more than 2^32 bytes whose last pages are used."""
     D, page, Hkv = 128, 1024, 8
