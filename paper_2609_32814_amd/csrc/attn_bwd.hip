@@ -35,7 +35,7 @@ __device__ __attribute__((aligned(256))) float g_attn_minus_inf[64] = {-INFINITY
 
 // NG groups of four wavefronts take the steps of the walk in turn, each with a
 // ring of its own; their sums meet at the end.
-template <int DH, int NG>
+template <int DH, int NG, int NB>
 __global__ __launch_bounds__(NG * kItemThreads, DH == 64 && NG == 1 ? 4 : 2) void attn_dq_kernel(const AttnBwdParams p) {
   constexpr int NCH = DH / 32, KS = DH / 16, TILE = tile_bytes<DH>(), NC = 2 * copies_per_step<DH>();
   extern __shared__ __attribute__((aligned(16))) char rings[];  // [group][stage][K, V]
@@ -80,13 +80,15 @@ __global__ __launch_bounds__(NG * kItemThreads, DH == 64 && NG == 1 ? 4 : 2) voi
   for (int x = 0; x < 4; ++x) ask(x);
   // the wave's rows of Q and dO as operands, delta and lse (asked for before
   // the first copies, used behind them)
+  const int m = DH / p.q;
+  const Blocks<DH, NB> bl(rec[3] & 0xffff, m);
   uint4 qf[KS], df[KS];
   uint4 of[2 * KS];  // O: 8 values in the first half of each pair, or fp32 in both
   const int64_t qrow = (seq0 + max(my, 0)) * ldq + h * DH;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     const int fr = 16 * ks + 8 * lh;
-    qf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.Q) + qrow + fr);
+    qf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.Q) + qrow + 16 * bl.turned(ks) + 8 * lh);
     df[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.dO) + qrow + fr);
   }
   if (p.odtype == 0) {
@@ -125,8 +127,8 @@ __global__ __launch_bounds__(NG * kItemThreads, DH == 64 && NG == 1 ? 4 : 2) voi
   Ends now, then;
   now.take(ring(0));
   then.take(ring(1));
-  now = now.settled();
-  then = then.settled();
+  now.settle();
+  then.settle();
 
   float delta = 0.f;
 #pragma unroll
@@ -165,8 +167,8 @@ __global__ __launch_bounds__(NG * kItemThreads, DH == 64 && NG == 1 ? 4 : 2) voi
       const char* Kt = tiles + st * 2 * TILE;
       tl.renew();
       f32x16_t sc{}, dp{};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) sc = mfma(tl.row(Kt, ks), qf[ks], sc);
+      const int j = wx.template block<DH, NB>(bl, m);
+      tl.template add_rows<NB>(sc, Kt, qf, bl, j);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) dp = mfma(tl.row(Kt + TILE, ks), df[ks], dp);
       // keys behind a query (rows past a type's end have position kNoPos)
@@ -187,11 +189,12 @@ __global__ __launch_bounds__(NG * kItemThreads, DH == 64 && NG == 1 ? 4 : 2) voi
 #pragma unroll
       for (int e = 0; e < 16; ++e) ds[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale2, -base)) * (dp[e] - delta);
       const uint4 pf[2] = {pack8(ds), pack8(ds + 8)};
-      tl.add_transposed(acc, Kt, pf);
+      tl.template add_transposed_kept<NB>(acc, Kt, pf, bl, j);
     }
     wx.next();
     now = then;
-    then = after.settled();
+    after.settle();
+    then = after;
   };
 
   for (int32_t n = 0; n < trips; n += 3) {
@@ -205,10 +208,10 @@ __global__ __launch_bounds__(NG * kItemThreads, DH == 64 && NG == 1 ? 4 : 2) voi
   if constexpr (NG == 2) {
     if (!join_groups<NCH>(acc, rings, g, wave, lane)) return;
   }
-  if (my >= 0) store_row<DH>(p.dQ, p.gdtype, qrow, acc, lh);
+  if (my >= 0) store_row<DH>(p.dQ, p.gdtype, qrow, acc, lh, bl.own * NB / 2);
 }
 
-template <int DH, int NG>
+template <int DH, int NG, int NB>
 __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_kernel(const AttnBwdParams p) {
   constexpr int NCH = DH / 32, KS = DH / 16, TILE = tile_bytes<DH>(), NC = 2 * copies_per_step<DH>();
   extern __shared__ __attribute__((aligned(16))) char rings[];  // [group][stage][Q, dO]
@@ -264,12 +267,14 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_k
     wc.next();
   };
   for (int x = 0; x < 4; ++x) ask(x);
+  const int m = DH / p.q;
+  const Blocks<DH, NB> bl(rec[3] & 0xffff, m);
   uint4 kf[KS], vf[KS];
   const int64_t krow = (seq0 + max(my, 0)) * ldk + hk * DH;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     const int fr = 16 * ks + 8 * lh;
-    kf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.K) + krow + fr);
+    kf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.K) + krow + 16 * bl.turned(ks) + 8 * lh);
     vf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.V) + krow + fr);
   }
   // positions ascend along the block: the first and last of the wave's rows
@@ -289,8 +294,8 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_k
   Ends now, then;
   now.take(ring(0));
   then.take(ring(1));
-  now = now.settled();
-  then = then.settled();
+  now.settle();
+  then.settle();
 
   // dk is kept in units of the walked type's scale
   f32x16_t dk[NCH], dv[NCH];
@@ -327,8 +332,8 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_k
         const float4 de = *reinterpret_cast<const float4*>(&side_s[st][32 + 8 * a + 4 * lh]);
         dp[4 * a] = de.x, dp[4 * a + 1] = de.y, dp[4 * a + 2] = de.z, dp[4 * a + 3] = de.w;
       }
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) sc = mfma(tl.row(Qt, ks), kf[ks], sc);
+      const int j = wx.template block<DH, NB>(bl, m);
+      tl.template add_rows<NB>(sc, Qt, kf, bl, j);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) dp = mfma(tl.row(Qt + TILE, ks), vf[ks], dp);
       if (now.first < tlast) {  // queries before a key
@@ -356,11 +361,12 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_k
       }
       const uint4 pf[2] = {pack8(pe), pack8(pe + 8)}, sf[2] = {pack8(ds), pack8(ds + 8)};
       tl.add_transposed(dv, Qt + TILE, pf);
-      tl.add_transposed(dk, Qt, sf);
+      tl.template add_transposed_kept<NB>(dk, Qt, sf, bl, j);
     }
     wx.next();
     now = then;
-    then = after.settled();
+    after.settle();
+    then = after;
   };
 
   for (int32_t n = 0; n < trips; n += 3) {
@@ -380,16 +386,16 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_k
     if (!join_groups<NCH>(dv, rings, g, wave, lane)) return;
   }
   if (my >= 0) {
-    store_row<DH>(p.dK, p.gdtype, krow, dk, lh);
+    store_row<DH>(p.dK, p.gdtype, krow, dk, lh, bl.own * NB / 2);
     store_row<DH>(p.dV, p.gdtype, krow, dv, lh);
   }
 }
 
-template <int DH, int NQ, int NK>
-hipError_t launch_groups(const AttnBwdParams& p, hipStream_t stream) {
+template <int DH, int NQ, int BQ, int NK, int BK>
+hipError_t launch_as(const AttnBwdParams& p, hipStream_t stream) {
   static std::atomic<unsigned long long> set_q{0}, set_k{0};
-  const auto dq = attn_dq_kernel<DH, NQ>;
-  const auto dkv = attn_dkv_kernel<DH, NK>;
+  const auto dq = attn_dq_kernel<DH, NQ, BQ>;
+  const auto dkv = attn_dkv_kernel<DH, NK, BK>;
   constexpr int smem = ring_bytes<DH>();
   hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(dq), set_q, NQ * smem);
   if (e != hipSuccess) return e;
@@ -403,21 +409,21 @@ hipError_t launch_groups(const AttnBwdParams& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <int DH, int NK>
-hipError_t launch_dh(const AttnBwdParams& p, hipStream_t stream) {
-  const bool few_q = pack_few(p.q_wgs, p.cus), few_k = NK == 2 || pack_few(p.k_wgs, p.cus);
-  if (few_q) return few_k ? launch_groups<DH, 2, 2>(p, stream) : launch_groups<DH, 2, NK>(p, stream);
-  return few_k ? launch_groups<DH, 1, 2>(p, stream) : launch_groups<DH, 1, NK>(p, stream);
-}
-
 }  // namespace
 
 hipError_t launch_attn_packed_bwd(const AttnBwdParams& p, hipStream_t stream) {
+  const bool few_q = pack_few(p.q_wgs, p.cus), few_k = pack_few(p.k_wgs, p.cus);
+  const int m = p.head_dim / p.q;
   switch (p.head_dim) {
-    // (head width 128: the registers hold two wavefronts of dK and dV a SIMD
-    // either way, and with two groups the longest walk is half as long)
-    case 64: return launch_dh<64, 1>(p, stream);
-    case 128: return launch_dh<128, 2>(p, stream);
+    case 64:
+      if (few_q || few_k) return few_q ? launch_as<64, 2, 0, 2, 0>(p, stream) : launch_as<64, 1, 0, 2, 0>(p, stream);
+      return blocks_fit<1>(p.law, p.q, m) ? launch_as<64, 1, 1, 1, 1>(p, stream) : launch_as<64, 1, 0, 1, 0>(p, stream);
+    case 128:
+      // dK and dV: two groups always (the registers hold two wavefronts of
+      // them a SIMD either way, and the longest walk is half as long)
+      if (few_q) return launch_as<128, 2, 0, 2, 0>(p, stream);
+      if (blocks_fit<2>(p.law, p.q, m)) return launch_as<128, 1, 2, 2, 2>(p, stream);
+      return blocks_fit<1>(p.law, p.q, m) ? launch_as<128, 1, 1, 2, 1>(p, stream) : launch_as<128, 1, 0, 2, 0>(p, stream);
     default: return hipErrorInvalidValue;
   }
 }

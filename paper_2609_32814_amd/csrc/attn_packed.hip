@@ -13,6 +13,8 @@
 //       transposing reads.
 // NG groups of wavefronts share the steps of one walk where there are few
 // work items; their states meet at the end.
+#include <cfloat>
+
 #include "attn_common.hpp"
 #include "attn_walk.hpp"
 
@@ -20,7 +22,7 @@ namespace starq {
 
 namespace {
 
-template <int DH, int NG>
+template <int DH, int NG, int NB>
 __global__ __launch_bounds__(NG * kItemThreads, NG == 2 ? 2 : DH == 64 ? 4 : 3) void attn_packed_fwd_kernel(const AttnParams p) {
   constexpr int NCH = DH / 32, KS = DH / 16, TILE = tile_bytes<DH>(), NC = 2 * copies_per_step<DH>();
   extern __shared__ __attribute__((aligned(16))) char rings[];  // [group][stage][K, V]
@@ -64,11 +66,13 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 2 ? 2 : DH == 64 ? 4 : 3) 
     wc.next();
   };
   for (int x = 0; x < 4; ++x) ask(x);
+  const int m = DH / p.q;
+  const Blocks<DH, NB> bl(rec[3] & 0xffff, m);
   uint4 qf[KS];
   const int64_t qrow = (seq0 + max(my, 0)) * ldq + h * DH;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks)
-    qf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.Q) + qrow + 16 * ks + 8 * lh);
+    qf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.Q) + qrow + 16 * bl.turned(ks) + 8 * lh);
   // positions ascend along the block: the first and last of the wave's rows
   const int32_t tv = min(32, nvalid - row0);
   const int32_t tfirst = tv > 0 ? uniform(my) : kNoPos;
@@ -85,13 +89,15 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 2 ? 2 : DH == 64 ? 4 : 3) 
   Ends now, then;
   now.take(ring(0));
   then.take(ring(1));
-  now = now.settled();
-  then = then.settled();
+  now.settle();
+  then.settle();
 
   f32x16_t acc[NCH];
 #pragma unroll
   for (int c = 0; c < NCH; ++c) acc[c] = f32x16_t{};
-  float run_max = -INFINITY, run_sum = 0.f;  // the sum over this lane's keys
+  // base 2; the maximum starts below every score, and finite (-inf - -inf is
+  // no number); the sum is over this lane's keys
+  float run_max = -FLT_MAX, run_sum = 0.f;
   TileLane<DH> tl(lane);
 
   // stage st: the tile of step `step`
@@ -106,10 +112,9 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 2 ? 2 : DH == 64 ? 4 : 3) 
     after.take(ring(step + 2));
     if (now.first <= tlast) {
       const char* Kt = tiles + st * 2 * TILE;
-      tl.renew();
+      if (DH == 128) tl.renew();
       f32x16_t sc{};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) sc = mfma(tl.row(Kt, ks), qf[ks], sc);
+      tl.template add_rows<NB>(sc, Kt, qf, bl, wx.template block<DH, NB>(bl, m));
       // keys behind a query (rows past a type's end have position kNoPos)
       if (now.last > tfirst) {
         const int32_t* kps = ring(step);
@@ -125,12 +130,12 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 2 ? 2 : DH == 64 ? 4 : 3) 
       float top = sc[0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) top = fmaxf(top, sc[e]);
-      const float scale2 = wx.scale * kLog2e;
-      top = max_xor32(top) * scale2;
       // the running maximum moves only by more than 8 at a time: until then
       // probabilities stay below 2^8
-      const bool need = top > run_max + 8.f;
-      if (__ballot(need) != 0) {
+      const float scale2 = wx.scale * kLog2e;
+      if (__ballot(__builtin_fmaf(top, scale2, -8.f) > run_max) != 0) {
+        top = max_xor32(top) * scale2;  // (both lanes of a query move alike)
+        const bool need = top > run_max + 8.f;
         const float corr = need ? __builtin_amdgcn_exp2f(run_max - top) : 1.f;
         if (need) run_max = top;
         run_sum *= corr;
@@ -139,11 +144,10 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 2 ? 2 : DH == 64 ? 4 : 3) 
 #pragma unroll
           for (int e = 0; e < 16; ++e) acc[c][e] *= corr;
       }
-      const float base = run_max == -INFINITY ? 0.f : run_max;
       float pe[16], sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        pe[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale2, -base));
+        pe[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale2, -run_max));
         sum += pe[e];
       }
       run_sum += sum;
@@ -152,7 +156,8 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 2 ? 2 : DH == 64 ? 4 : 3) 
     }
     wx.next();
     now = then;
-    then = after.settled();
+    after.settle();
+    then = after;
   };
 
   for (int32_t n = 0; n < trips; n += 3) {
@@ -172,17 +177,15 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 2 ? 2 : DH == 64 ? 4 : 3) 
     __syncthreads();
     const float m1 = state_s[wave][lane][0], l1 = state_s[wave][lane][1];
     __syncthreads();
-    if (g == 0) {
-      state_s[wave][lane][0] = run_max;
-    }
+    if (g == 0) state_s[wave][lane][0] = run_max;
     __syncthreads();
     const float mx = fmaxf(state_s[wave][lane][0], m1);
-    const float corr = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(run_max - mx);
+    const float corr = __builtin_amdgcn_exp2f(run_max - mx);
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[c][e] *= corr;
-    run_sum = run_sum * corr + (mx == -INFINITY ? 0.f : l1 * __builtin_amdgcn_exp2f(m1 - mx));  // (of use in the first group)
+    run_sum = run_sum * corr + l1 * __builtin_amdgcn_exp2f(m1 - mx);  // (of use in the first group)
     run_max = mx;
     if (!join_groups<NCH>(acc, rings, g, wave, lane)) return;
   }
@@ -199,14 +202,15 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 2 ? 2 : DH == 64 ? 4 : 3) 
   }
 }
 
-template <int DH, int NG>
+template <int DH, int NG, int NB>
 hipError_t launch(const AttnParams& p, hipStream_t stream) {
   static std::atomic<unsigned long long> set{0};
-  const auto fn = attn_packed_fwd_kernel<DH, NG>;
-  hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(fn), set, NG * ring_bytes<DH>());
+  const auto fn = attn_packed_fwd_kernel<DH, NG, NB>;
+  constexpr int smem = NG * ring_bytes<DH>();
+  hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(fn), set, smem);
   if (e != hipSuccess) return e;
   const unsigned grid = static_cast<unsigned>(p.main_wgs + pack_clear_wgs(p.S));
-  hipLaunchKernelGGL(fn, dim3(grid), dim3(NG * kItemThreads), NG * ring_bytes<DH>(), stream, p);
+  hipLaunchKernelGGL(fn, dim3(grid), dim3(NG * kItemThreads), smem, stream, p);
   return hipGetLastError();
 }
 
@@ -214,9 +218,15 @@ hipError_t launch(const AttnParams& p, hipStream_t stream) {
 
 hipError_t launch_attn_packed_fwd(const AttnParams& p, hipStream_t stream) {
   const bool few = pack_few(p.main_wgs, p.cus);
+  const int m = p.head_dim / p.q;
   switch (p.head_dim) {
-    case 64: return few ? launch<64, 2>(p, stream) : launch<64, 1>(p, stream);
-    case 128: return few ? launch<128, 2>(p, stream) : launch<128, 1>(p, stream);
+    case 64:
+      if (few) return launch<64, 2, 0>(p, stream);
+      return blocks_fit<1>(p.law, p.q, m) ? launch<64, 1, 1>(p, stream) : launch<64, 1, 0>(p, stream);
+    case 128:
+      if (few) return launch<128, 2, 0>(p, stream);
+      if (blocks_fit<2>(p.law, p.q, m)) return launch<128, 1, 2>(p, stream);
+      return blocks_fit<1>(p.law, p.q, m) ? launch<128, 1, 1>(p, stream) : launch<128, 1, 0>(p, stream);
     default: return hipErrorInvalidValue;
   }
 }

@@ -1,6 +1,7 @@
 // The walk of a pack's work item (see PackView in kernels.hpp): rows of two
-// [T][heads][DH] arrays, type by type, 32 rows a step, brought into a ring of
-// three LDS tiles of either array by direct copies two steps ahead of their use.
+// [T][heads][DH] arrays, type by type, 32 rows a step, brought into a ring
+// of three LDS tiles of either array by direct copies two steps ahead of their
+// use.
 //
 // A group of four wavefronts goes through step h like this (the kernels' loop
 // body h):
@@ -22,7 +23,7 @@ namespace starq {
 
 namespace {
 
-constexpr int kStep = 32;     // rows per step
+constexpr int kStep = 32;
 constexpr int kStages = 3;    // tiles of either array
 constexpr int kPosSlots = 8;  // steps whose positions are held
 constexpr int32_t kNoPos = 0x7fffffff;
@@ -54,10 +55,29 @@ __device__ __forceinline__ uint4 pack8(const float* v) {
   return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
 
+// Of a pair of types the star law keeps two groups.  NB > 0: features in blocks
+// of 16 NB, each holding whole groups or lying in one, so that a pair keeps at
+// most two blocks, the item's own and the walked type's, and the products can
+// leave the others out; blocks are counted from the item's own one on (the
+// walked block is picked by uniform branches around its products, its rows
+// by their address).  NB = 0: all features, zeros where a pair keeps none.
+template <int DH, int NB>
+struct Blocks {
+  static constexpr int KS = DH / 16, N = NB > 0 ? KS / NB : 1;
+  int own;  // block of the item's type
+  __device__ __forceinline__ Blocks(int type, int m) : own(NB > 0 ? type * m / (16 * (NB > 0 ? NB : 1)) : 0) {}
+  // turn-th 16 features from the own block on
+  __device__ __forceinline__ int turned(int ks) const { return NB > 0 ? ((own * NB) + ks) % KS : ks; }
+};
+template <int NB>
+inline bool blocks_fit(int law, int q, int m) {
+  return NB == 0 || (law == 0 && q >= 4 && (m >= 32 ? NB == 2 : NB == 1));
+}
+
 // What a work item's walk needs per type.
 template <int NG>
 struct ItemLds {
-  int32_t ring[NG][kPosSlots][64];         // per group: positions of the walked rows (32 used), kNoPos past a type's end
+  int32_t ring[NG][kPosSlots][64];         // per group: positions of the walked rows (the first 32), kNoPos past a type's end
   int32_t off[kAttnMaxQ], cnt[kAttnMaxQ];  // the walked range of the pack's permutation
   uint32_t cells[kAttnMaxQ];               // 8-feature cells that its pairs with the item's type keep
   float scale[kAttnMaxQ], lg[kAttnMaxQ];   // their scale and its logarithm (base 2)
@@ -123,6 +143,11 @@ struct Walk {
     for (int x = 0; x < NG; ++x) step();
   }
   __device__ __forceinline__ bool done() const { return hh >= heads; }
+  // the walked type's block, counted from the item's own
+  template <int DH, int NB>
+  __device__ __forceinline__ int block(const Blocks<DH, NB>& bl, int m) const {
+    return NB > 0 ? (j * m / (16 * (NB > 0 ? NB : 1)) - bl.own + Blocks<DH, NB>::N) % Blocks<DH, NB>::N : 0;
+  }
   // steps of the first group, which has the most (a group that is done goes
   // on with empty ones)
   __device__ __forceinline__ int32_t trips() const {
@@ -135,7 +160,7 @@ struct Walk {
 // Wavefront 0: the positions of a step into a slot of the ring.
 template <int NG>
 __device__ __forceinline__ void ask_positions(const Walk<NG>& w, const int32_t* perm, int32_t* slot, int lane) {
-  const int32_t r = w.c + (lane & 31);
+  const int32_t r = w.c + (lane & (kStep - 1));
   dma4(!w.done() && r < w.rows ? perm + w.base + r : g_attn_no_pos, lds_addr(slot));
 }
 
@@ -163,12 +188,12 @@ struct Copies {
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       const int r = row(k, wave, lane), c = (lane % CPR) ^ swz<DH>(r);
-      const bool ok = pos[k] != kNoPos;
-      const uint64_t at = static_cast<uint64_t>(__umul24(pos[k], stride16) + c) << 4;
-      const uint64_t a = reinterpret_cast<uint64_t>(A) + at, b = reinterpret_cast<uint64_t>(B) + at;
+      const uint64_t at = static_cast<uint64_t>(static_cast<uint32_t>(__umul24(pos[k], stride16)) + static_cast<uint32_t>(c)) << 4;
+      const bool ok = pos[k] != kNoPos, kept = ok & (((cells >> c) & 1u) != 0);
+      const uint64_t a = kept ? reinterpret_cast<uint64_t>(A) + at : zero, b = ok ? reinterpret_cast<uint64_t>(B) + at : zero;
       char* to = stage + (wave + kItemWaves * k) * 1024;
-      dma16(reinterpret_cast<const void*>(ok && ((cells >> c) & 1u) ? a : zero), lds_addr(to));
-      dma16(reinterpret_cast<const void*>(ok ? b : zero), lds_addr(to + tile_bytes<DH>()));
+      dma16(reinterpret_cast<const void*>(a), lds_addr(to));
+      dma16(reinterpret_cast<const void*>(b), lds_addr(to + tile_bytes<DH>()));
     }
   }
 };
@@ -180,7 +205,10 @@ struct Ends {
     first = slot[0];
     last = slot[kStep - 1];
   }
-  __device__ __forceinline__ Ends settled() const { return {uniform(first), uniform(last)}; }
+  __device__ __forceinline__ void settle() {
+    first = uniform(first);
+    last = uniform(last);
+  }
 };
 
 template <int N>
@@ -233,6 +261,48 @@ struct TileLane {
     const uint2 w1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((STARQ_LDS v4i16_t*)(a1)));
     return make_uint4(w0.x, w0.y, w1.x, w1.y);
   }
+  // sum += rows of `tile` x ops, ops counted from the own block on; j: the
+  // walked type's block, counted likewise
+  template <int NB>
+  __device__ __forceinline__ void add_rows(f32x16_t& sum, const char* tile, const uint4* ops, const Blocks<DH, NB>& bl, int j) const {
+    constexpr int N = Blocks<DH, NB>::N, B = NB > 0 ? NB : DH / 16;
+#pragma unroll
+    for (int x = 0; x < B; ++x) sum = mfma(row(tile, bl.turned(x)), ops[x], sum);
+    if constexpr (NB > 0) {
+      uint4 f[B];
+#pragma unroll
+      for (int x = 0; x < B; ++x) f[x] = row(tile, bl.turned(j * NB + x));
+#pragma unroll
+      for (int r = 1; r < N; ++r)
+        if (j == r) {
+#pragma unroll
+          for (int x = 0; x < B; ++x) sum = mfma(f[x], ops[r * NB + x], sum);
+        }
+    }
+  }
+  // acc += (rows of `tile`)^T x ops of the blocks that a pair keeps, in chunks
+  // of 32 features counted from the own block's on
+  template <int NB>
+  __device__ __forceinline__ void add_transposed_kept(f32x16_t* acc, const char* tile, const uint4* ops, const Blocks<DH, NB>& bl,
+                                                      int j) const {
+    if constexpr (NB == 0) {
+      add_transposed(acc, tile, ops);
+    } else {
+      constexpr int NCH = DH / 32;
+      const int c0 = bl.own * NB / 2, c1 = bl.turned(j * NB) / 2, r1 = (c1 - c0 + NCH) % NCH;
+#pragma unroll
+      for (int kk = 0; kk < kStep / 16; ++kk) acc[0] = mfma(transposed(tile, kk, c0), ops[kk], acc[0]);
+      uint4 f[kStep / 16];
+#pragma unroll
+      for (int kk = 0; kk < kStep / 16; ++kk) f[kk] = transposed(tile, kk, c1);
+#pragma unroll
+      for (int r = 1; r < NCH; ++r)
+        if (r1 == r) {
+#pragma unroll
+          for (int kk = 0; kk < kStep / 16; ++kk) acc[r] = mfma(f[kk], ops[kk], acc[r]);
+        }
+    }
+  }
   // acc += (rows of `tile`)^T x ops, ops[kk] the operand of rows 16 kk and on
   __device__ __forceinline__ void add_transposed(f32x16_t* acc, const char* tile, const uint4* ops) const {
 #pragma unroll
@@ -266,13 +336,14 @@ __device__ __forceinline__ bool join_groups(f32x16_t* acc, char* rings, int g, i
 
 // Rows of a transposed product's result: acc[c][4 a + e] is feature
 // 32 c + 8 a + 4 (l / 32) + e of the lane's row.
+// (first: the chunk that acc[0] is of)
 template <int DH>
-__device__ __forceinline__ void store_row(void* out, int dtype, int64_t at, const f32x16_t* acc, int lh) {
+__device__ __forceinline__ void store_row(void* out, int dtype, int64_t at, const f32x16_t* acc, int lh, int first = 0) {
 #pragma unroll
   for (int c = 0; c < DH / 32; ++c)
 #pragma unroll
     for (int a = 0; a < 4; ++a) {
-      const int f = 32 * c + 8 * a + 4 * lh;
+      const int f = 32 * ((c + first) % (DH / 32)) + 8 * a + 4 * lh;
       const float v0 = acc[c][4 * a], v1 = acc[c][4 * a + 1], v2 = acc[c][4 * a + 2], v3 = acc[c][4 * a + 3];
       if (dtype == 0)
         *reinterpret_cast<float4*>(static_cast<float*>(out) + at + f) = make_float4(v0, v1, v2, v3);

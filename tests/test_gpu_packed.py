@@ -92,6 +92,21 @@ CASES = [
     ("star", 4, 128, 8, 1, [333, 2], "random"),       # eight query heads on one
     ("star", 2, 128, 6, 2, [700], None),
     ("star", 4, 64, 3, 1, [1025], "random"),
+    # many heads: one group of wavefronts per work item, and the star law's
+    # kernels that leave feature blocks out
+    ("dense", 1, 64, 72, 72, [200, 77], None),
+    ("tensor2", 4, 64, 72, 72, [330], "interval"),
+    ("star", 2, 64, 72, 72, [150, 1], "random"),
+    ("star", 4, 64, 72, 72, [150, 99], "random"),
+    ("star", 8, 64, 72, 72, [190], "random"),
+    ("star", 4, 64, 72, 8, [170, 40], None),
+    ("dense", 1, 128, 64, 64, [140, 70], None),
+    ("star", 2, 128, 64, 16, [200, 33], None),
+    ("star", 4, 128, 64, 64, [150, 130], "random"),
+    ("star", 4, 128, 64, 8, [260, 2], None),
+    ("star", 8, 128, 64, 64, [170, 65], "random"),
+    ("star", 16, 128, 64, 64, [260], "random"),
+    ("star", 4, 64, 72, 72, [140, 50, 9], "some_bad"),
     ("star", 4, 64, 2, 2, [140, 50, 9], "some_bad"),
     ("dense", 1, 128, 2, 2, [100, 3], "some_bad"),
 ]
