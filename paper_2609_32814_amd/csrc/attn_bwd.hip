@@ -23,6 +23,8 @@
 //
 // P and dS enter their products rounded to bf16 (at most 2^-9 of each term,
 // like the operands themselves); everything else is fp32.
+#include <type_traits>
+
 #include "attn_common.hpp"
 #include "attn_walk.hpp"
 
@@ -30,8 +32,9 @@ namespace starq {
 
 namespace {
 
-// -inf for the log-sum-exp of a row that is not there: its probabilities are zero
-__device__ __attribute__((aligned(256))) float g_attn_minus_inf[64] = {-INFINITY};
+// For a row that is not there: -inf for its negated log-sum-exp, so that its
+// probabilities are zero, and zero for its delta
+__device__ __attribute__((aligned(256))) float g_attn_no_side[2] = {-INFINITY, 0.f};
 
 // NG groups of four wavefronts take the steps of the walk in turn, each with a
 // ring of its own; their sums meet at the end.
@@ -117,18 +120,21 @@ __global__ __launch_bounds__(NG * kItemThreads, DH == 64 && NG == 1 ? 4 : 2) voi
   landed(of, my >= 0);
   landed(lse2);
   lse2 = my >= 0 ? lse2 * kLog2e : 0.f;
-  __syncthreads();
-  cp.take(ring(0), wave, lane);
-  copy(0);
-  cp.take(ring(1), wave, lane);
-  ask(4);
-  copy(1);
-  cp.take(ring(2), wave, lane);
   Ends now, then;
-  now.take(ring(0));
-  then.take(ring(1));
-  now.settle();
-  then.settle();
+  auto start = [&] {
+    __syncthreads();
+    cp.take(ring(0), wave, lane);
+    copy(0);
+    cp.take(ring(1), wave, lane);
+    ask(4);
+    copy(1);
+    cp.take(ring(2), wave, lane);
+    now.take(ring(0));
+    then.take(ring(1));
+    now.settle();
+    then.settle();
+  };
+  start();
 
   float delta = 0.f;
 #pragma unroll
@@ -154,7 +160,9 @@ __global__ __launch_bounds__(NG * kItemThreads, DH == 64 && NG == 1 ? 4 : 2) voi
   TileLane<DH> tl(lane);
 
   // stage st: the tile of step `step`
-  auto body = [&](int st, int32_t step) {
+  const std::true_type yes;
+  const std::false_type no;
+  auto body = [&](auto care, int st, int32_t step) {
     if (wave == 0) wait_vm<NC + 1>();
     else wait_vm<NC>();
     __syncthreads();
@@ -177,10 +185,13 @@ __global__ __launch_bounds__(NG * kItemThreads, DH == 64 && NG == 1 ? 4 : 2) voi
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
           const int4 kq = *reinterpret_cast<const int4*>(kps + 8 * a + 4 * lh);
-          if (kq.x > my) sc[4 * a + 0] = -INFINITY;
-          if (kq.y > my) sc[4 * a + 1] = -INFINITY;
-          if (kq.z > my) sc[4 * a + 2] = -INFINITY;
-          if (kq.w > my) sc[4 * a + 3] = -INFINITY;
+          const int32_t k4[4] = {kq.x, kq.y, kq.z, kq.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (k4[e] > my) {
+              sc[4 * a + e] = -INFINITY;
+              if (care) dp[4 * a + e] = delta;
+            }
         }
       }
       // dS = scale P (dP - delta): the scale goes into the exponent
@@ -189,7 +200,8 @@ __global__ __launch_bounds__(NG * kItemThreads, DH == 64 && NG == 1 ? 4 : 2) voi
 #pragma unroll
       for (int e = 0; e < 16; ++e) ds[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], scale2, -base)) * (dp[e] - delta);
       const uint4 pf[2] = {pack8(ds), pack8(ds + 8)};
-      tl.template add_transposed_kept<NB>(acc, Kt, pf, bl, j);
+      if (care) tl.add_odd(acc, Kt, pf, bl.own * NB / 2);
+      else tl.template add_transposed_kept<NB>(acc, Kt, pf, bl, j);
     }
     wx.next();
     now = then;
@@ -198,13 +210,24 @@ __global__ __launch_bounds__(NG * kItemThreads, DH == 64 && NG == 1 ? 4 : 2) voi
   };
 
   for (int32_t n = 0; n < trips; n += 3) {
-    body(0, n);
+    body(no, 0, n);
     if (n + 1 == trips) break;
-    body(1, n + 1);
+    body(no, 1, n + 1);
     if (n + 2 == trips) break;
-    body(2, n + 2);
+    body(no, 2, n + 2);
   }
   wait_vm<0>();
+  if (__syncthreads_or(odd(acc))) {
+    wx = wp = wc = Walk<NG>(&it_s, p.q, 1, g);
+    for (int x = 0; x < 4; ++x) ask(x);
+    wait_vm<0>();
+    start();
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) acc[c] = f32x16_t{};
+#pragma unroll 1
+    for (int32_t n = 0; n < trips; ++n) body(yes, n % kStages, n);
+    wait_vm<0>();
+  }
   if constexpr (NG == 2) {
     if (!join_groups<NCH>(acc, rings, g, wave, lane)) return;
   }
@@ -258,11 +281,18 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_k
     side_pos = ring(step)[lr];
   };
   // rows, and by wavefront 1 their log-sum-exps and deltas
-  const float* side0 = p.side + (static_cast<int64_t>(lh) * p.n_heads + hk * rep) * p.T + seq0;
-  const float* no_side = lh == 0 ? g_attn_minus_inf : reinterpret_cast<const float*>(cp.zero);
+  const float* side0 = p.side + static_cast<int64_t>(hk) * rep * p.T + seq0;
+  const float* no_side = g_attn_no_side;
+  asm volatile("" : "+s"(no_side));
   auto copy = [&](int st) {
-    if (wave == 1)
-      dma4(side_pos != kNoPos ? side0 + static_cast<int64_t>(wc.hh) * p.T + side_pos : no_side, lds_addr(side_s[st]));
+    if (wave == 1) {
+      int half = lane;
+      asm volatile("" : "+v"(half));  // (worth no register between the steps)
+      half >>= 5;
+      const float* row = side0 + static_cast<int64_t>(wc.hh) * p.T;
+      const float* at = row + (half ? static_cast<int64_t>(p.n_heads) * p.T : 0) + side_pos;
+      dma4(side_pos != kNoPos ? at : no_side + half, lds_addr(side_s[st]));
+    }
     cp.issue(Qg + wc.hh * DH, Dg + wc.hh * DH, ldq16, wc.cells, tiles + st * 2 * TILE, wave, lane);
     wc.next();
   };
@@ -270,13 +300,19 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_k
   const int m = DH / p.q;
   const Blocks<DH, NB> bl(rec[3] & 0xffff, m);
   uint4 kf[KS], vf[KS];
-  const int64_t krow = (seq0 + max(my, 0)) * ldk + hk * DH;
+  auto krow = [&] {  // (worth no registers between its uses)
+    int32_t r = max(my, 0);
+    asm volatile("" : "+v"(r));
+    return (seq0 + r) * ldk + hk * DH;
+  };
+  auto operands = [&](int64_t row) {
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {
-    const int fr = 16 * ks + 8 * lh;
-    kf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.K) + krow + 16 * bl.turned(ks) + 8 * lh);
-    vf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.V) + krow + fr);
-  }
+    for (int ks = 0; ks < KS; ++ks) {
+      kf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.K) + row + 16 * bl.turned(ks) + 8 * lh);
+      vf[ks] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.V) + row + 16 * ks + 8 * lh);
+    }
+  };
+  operands(krow());
   // positions ascend along the block: the first and last of the wave's rows
   const int32_t tv = min(32, nvalid - row0);
   const int32_t tfirst = tv > 0 ? uniform(my) : kNoPos;
@@ -284,18 +320,21 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_k
   wait_vm<0>();
   landed(kf, my >= 0);
   landed(vf, my >= 0);
-  __syncthreads();
-  take(0);
-  copy(0);
-  take(1);
-  ask(4);
-  copy(1);
-  take(2);
   Ends now, then;
-  now.take(ring(0));
-  then.take(ring(1));
-  now.settle();
-  then.settle();
+  auto start = [&] {
+    __syncthreads();
+    take(0);
+    copy(0);
+    take(1);
+    ask(4);
+    copy(1);
+    take(2);
+    now.take(ring(0));
+    then.take(ring(1));
+    now.settle();
+    then.settle();
+  };
+  start();
 
   // dk is kept in units of the walked type's scale
   f32x16_t dk[NCH], dv[NCH];
@@ -304,7 +343,9 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_k
   float unit = wx.scale;
   TileLane<DH> tl(lane);
 
-  auto body = [&](int st, int32_t step) {
+  const std::true_type yes;
+  const std::false_type no;
+  auto body = [&](auto care, int st, int32_t step) {
     if (wave < 2) wait_vm<NC + 1>();
     else wait_vm<NC>();
     __syncthreads();
@@ -359,9 +400,19 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_k
           ds[4 * a + e] = pe[4 * a + e] * dp[4 * a + e];
         }
       }
+      if (care && now.first < tlast) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (sc[e] == -INFINITY) pe[e] = ds[e] = 0.f;
+      }
       const uint4 pf[2] = {pack8(pe), pack8(pe + 8)}, sf[2] = {pack8(ds), pack8(ds + 8)};
-      tl.add_transposed(dv, Qt + TILE, pf);
-      tl.template add_transposed_kept<NB>(dk, Qt, sf, bl, j);
+      if (care) {
+        tl.add_odd(dv, Qt + TILE, pf);
+        tl.add_odd(dk, Qt, sf, bl.own * NB / 2);
+      } else {
+        tl.add_transposed(dv, Qt + TILE, pf);
+        tl.template add_transposed_kept<NB>(dk, Qt, sf, bl, j);
+      }
     }
     wx.next();
     now = then;
@@ -370,13 +421,28 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_k
   };
 
   for (int32_t n = 0; n < trips; n += 3) {
-    body(0, n);
+    body(no, 0, n);
     if (n + 1 == trips) break;
-    body(1, n + 1);
+    body(no, 1, n + 1);
     if (n + 2 == trips) break;
-    body(2, n + 2);
+    body(no, 2, n + 2);
   }
   wait_vm<0>();
+  if (__syncthreads_or(odd(dk) || odd(dv))) {
+    wx = wp = wc = Walk<NG>(&it_s, p.q, rep, g);
+    for (int x = 0; x < 4; ++x) ask(x);
+    operands(krow());  // (held for this they would cost the first walk registers)
+    wait_vm<0>();
+    landed(kf, my >= 0);
+    landed(vf, my >= 0);
+    start();
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) dk[c] = dv[c] = f32x16_t{};
+    unit = wx.scale;
+#pragma unroll 1
+    for (int32_t n = 0; n < trips; ++n) body(yes, n % kStages, n);
+    wait_vm<0>();
+  }
 #pragma unroll
   for (int c = 0; c < NCH; ++c)
 #pragma unroll
@@ -386,8 +452,9 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_k
     if (!join_groups<NCH>(dv, rings, g, wave, lane)) return;
   }
   if (my >= 0) {
-    store_row<DH>(p.dK, p.gdtype, krow, dk, lh, bl.own * NB / 2);
-    store_row<DH>(p.dV, p.gdtype, krow, dv, lh);
+    const int64_t row = krow();
+    store_row<DH>(p.dK, p.gdtype, row, dk, lh, bl.own * NB / 2);
+    store_row<DH>(p.dV, p.gdtype, row, dv, lh);
   }
 }
 

@@ -14,6 +14,7 @@
 // NG groups of wavefronts share the steps of one walk where there are few
 // work items; their states meet at the end.
 #include <cfloat>
+#include <type_traits>
 
 #include "attn_common.hpp"
 #include "attn_walk.hpp"
@@ -79,18 +80,21 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 2 ? 2 : DH == 64 ? 4 : 3) 
   const int32_t tlast = tv > 0 ? __builtin_amdgcn_readlane(my, tv - 1) : -1;
   wait_vm<0>();
   landed(qf, my >= 0);
-  __syncthreads();
-  cp.take(ring(0), wave, lane);
-  copy(0);
-  cp.take(ring(1), wave, lane);
-  ask(4);
-  copy(1);
-  cp.take(ring(2), wave, lane);
   Ends now, then;
-  now.take(ring(0));
-  then.take(ring(1));
-  now.settle();
-  then.settle();
+  auto start = [&] {
+    __syncthreads();
+    cp.take(ring(0), wave, lane);
+    copy(0);
+    cp.take(ring(1), wave, lane);
+    ask(4);
+    copy(1);
+    cp.take(ring(2), wave, lane);
+    now.take(ring(0));
+    then.take(ring(1));
+    now.settle();
+    then.settle();
+  };
+  start();
 
   f32x16_t acc[NCH];
 #pragma unroll
@@ -101,7 +105,9 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 2 ? 2 : DH == 64 ? 4 : 3) 
   TileLane<DH> tl(lane);
 
   // stage st: the tile of step `step`
-  auto body = [&](int st, int32_t step) {
+  const std::true_type yes;
+  const std::false_type no;
+  auto body = [&](auto care, int st, int32_t step) {
     if (wave == 0) wait_vm<NC + 1>();
     else wait_vm<NC>();
     __syncthreads();
@@ -152,7 +158,8 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 2 ? 2 : DH == 64 ? 4 : 3) 
       }
       run_sum += sum;
       const uint4 pf[2] = {pack8(pe), pack8(pe + 8)};
-      tl.add_transposed(acc, Kt + TILE, pf);
+      if (care) tl.add_odd(acc, Kt + TILE, pf);
+      else tl.add_transposed(acc, Kt + TILE, pf);
     }
     wx.next();
     now = then;
@@ -161,13 +168,25 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 2 ? 2 : DH == 64 ? 4 : 3) 
   };
 
   for (int32_t n = 0; n < trips; n += 3) {
-    body(0, n);
+    body(no, 0, n);
     if (n + 1 == trips) break;
-    body(1, n + 1);
+    body(no, 1, n + 1);
     if (n + 2 == trips) break;
-    body(2, n + 2);
+    body(no, 2, n + 2);
   }
   wait_vm<0>();
+  if (__syncthreads_or(odd(acc))) {
+    wx = wp = wc = Walk<NG>(&it_s, p.q, 1, g);
+    for (int x = 0; x < 4; ++x) ask(x);
+    wait_vm<0>();
+    start();
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) acc[c] = f32x16_t{};
+    run_max = -FLT_MAX, run_sum = 0.f;
+#pragma unroll 1
+    for (int32_t n = 0; n < trips; ++n) body(yes, n % kStages, n);
+    wait_vm<0>();
+  }
   run_sum = sum_xor32(run_sum);
   if constexpr (NG == 2) {  // both groups in units of the larger maximum
     if (g == 1) {

@@ -310,7 +310,67 @@ struct TileLane {
 #pragma unroll
       for (int c = 0; c < DH / 32; ++c) acc[c] = mfma(transposed(tile, kk, c), ops[kk], acc[c]);
   }
+  // Masked places enter the products above with weight zero, and zero times an
+  // infinity is no number.  The same sums in parts: of the finite values, and
+  // for each feature whether an infinity (or a value that is no number: both
+  // signs) meets a weight.  first: the chunk that acc[0] is of
+  __device__ __forceinline__ void add_odd(f32x16_t* acc, const char* tile, const uint4* ops, int first = 0) const {
+    // (rare, so in the order that takes the fewest registers)
+#pragma unroll
+    for (int c = 0; c < DH / 32; ++c) {
+      const int chunk = (c + first) % (DH / 32);
+#pragma unroll
+      for (int kk = 0; kk < kStep / 16; ++kk) {
+        acc[c] = mfma(picked(transposed(tile, kk, chunk), 0), ops[kk], acc[c]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int sign = 1; sign >= -1; sign -= 2) {
+        f32x16_t met{};
+#pragma unroll
+        for (int kk = 0; kk < kStep / 16; ++kk) {
+          const uint4 w = ops[kk];
+          met = mfma(picked(transposed(tile, kk, chunk), sign),
+                     make_uint4(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu, w.z & 0x7fff7fffu, w.w & 0x7fff7fffu), met);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[c][e] += met[e] > 0.f ? sign * __builtin_inff() : 0.f;
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  // which 0: the finite ones of 8 bf16 values, zeros for others; which 1 or -1:
+  // ones where there is an infinity of that sign or no number
+  __device__ __forceinline__ static uint32_t picked(uint32_t x, int which) {
+    uint32_t r = 0;
+#pragma unroll
+    for (int half = 0; half < 32; half += 16) {
+      const uint32_t v = (x >> half) & 0xffffu;
+      const bool there = (v & 0x7f80u) == 0x7f80u;
+      r |= (which == 0 ? (there ? 0u : v) : there && v != (which > 0 ? 0xff80u : 0x7f80u) ? 0x3f80u : 0u) << half;
+    }
+    return r;
+  }
+  __device__ __forceinline__ static uint4 picked(uint4 x, int which) {
+    return make_uint4(picked(x.x, which), picked(x.y, which), picked(x.z, which), picked(x.w, which));
+  }
 };
+
+// Whether any of a wavefront's sums is not finite: if so its workgroup walks a
+// second time (`care`), one step's code for all three stages, with add_odd and
+// with nothing left of masked places.  The loop that everyone runs stays as it
+// is: testing the tiles that hold masked places there, or two ways to add in
+// it, cost 4 to 22 % (the registers are full); so placed it costs 0 to 3 %.
+template <int N>
+__device__ __forceinline__ bool odd(const f32x16_t (&acc)[N]) {
+  float s = 0.f;
+#pragma unroll
+  for (int c = 0; c < N; ++c)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s = __builtin_fmaf(acc[c][e], 0.f, s);
+  return s != 0.f;  // zero, or no number
+}
 
 // The second group's sums added to the first's, through LDS where the rings
 // were.  True in the first group.

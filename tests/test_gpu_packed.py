@@ -264,3 +264,73 @@ def test_side_stream_and_graph_replays(P):
         for x, y in zip(outs, (O, lse, *src.bwd(O, lse))):
             assert torch.equal(x, y)
     assert torch.equal(warm[0], a.fwd())
+
+
+ODD = [
+    ("dense", 1, 64, 2, 2, [150, 70], None),
+    ("star", 4, 64, 2, 1, [200, 30], "random"),
+    ("tensor2", 2, 128, 4, 2, [140, 31], None),
+    ("star", 4, 64, 72, 72, [160, 40], None),
+    ("star", 4, 128, 64, 16, [170], "random"),
+    ("dense", 1, 128, 64, 64, [140], None),
+    ("star", 2, 64, 6, 2, [131], "some_bad"),
+]
+
+
+@pytest.mark.parametrize("law,q,D,H,Hkv,lens,types", ODD)
+@pytest.mark.parametrize("t", [0, 37, 129])
+def test_what_is_not_finite_stays_out_of_masked_places(P, law, q, D, H, Hkv, lens, types, t):
+    """A position with infinities and NaN reaches neither the earlier positions
+    of its sequence nor another sequence: their weights of it are none, and
+    not zero times it.  Values of V that are infinite or NaN reach their own
+    feature alone."""
+    c = Pack(P, law, q, D, H, Hkv, lens, seed=5, types=types)
+    c.types[t] = 0
+    c.d["types"] = c.types.to(DEV)
+    c.pack = P.star_attn_pack(q, c.d["types"], c.dcu)
+    keep = torch.ones(c.T, dtype=torch.bool)
+    keep[t:lens[0]] = False  # rows that may not see position t
+    O, lse = c.fwd(out_dtype=F32, want_lse=True)
+    rO, rl, mag = ref.forward(law, q, c.types, c.cu, c.Q, c.K, c.V)
+    bar = (ref.HALF + ref.SLACK) * mag
+
+    # V: features 3 (infinite), 20 (minus), 21 (NaN)
+    V = c.V.clone()
+    V[t, :, 3], V[t, :, 20], V[t, :, 21] = torch.inf, -torch.inf, torch.nan
+    c.d["V"] = V.to(DEV)
+    O1, l1 = c.fwd(out_dtype=F32, want_lse=True)
+    rest = [f for f in range(D) if f not in (3, 20, 21)]
+    assert ref.off(O1[:, :, rest], rO[:, :, rest], bar[:, :, rest], False) <= 1
+    assert ref.off(O1[keep.to(DEV)], rO[keep], bar[keep], False) <= 1
+    assert torch.equal(l1, lse)
+    hit = (~keep & ref.valid(c.types, q)).to(DEV)
+    assert bool(torch.isposinf(O1[hit][:, :, 3]).all()) and bool(torch.isneginf(O1[hit][:, :, 20]).all())
+    assert bool(torch.isnan(O1[hit][:, :, 21]).all())
+
+    # K too: dQ of the rows that do not see it
+    K = c.K.clone()
+    K[t, :, ::5], K[t, :, 1::5] = torch.nan, torch.inf
+    c.d["K"] = K.to(DEV)
+    O2, l2 = c.fwd(out_dtype=F32, want_lse=True)
+    assert ref.off(O2[keep.to(DEV)], rO[keep], bar[keep], False) <= 1
+    dQ = c.bwd(O2, l2, out_dtype=F32)[0]
+    ko, kl = keep[:, None, None], keep[None, :]
+    rg, bars = ref.backward(law, q, c.types, c.cu, c.dO, c.Q, c.K, c.V, torch.where(ko, O2.cpu(), O.cpu()),
+                            torch.where(kl, l2.cpu(), lse.cpu()))
+    assert ref.off(dQ[keep.to(DEV)], rg[0][keep], bars[0][keep], False) <= 1
+
+    # Q and dO: dK and dV of the keys that it does not see
+    c.d["K"], c.d["V"] = c.K.to(DEV), c.V.to(DEV)
+    Q, dO = c.Q.clone(), c.dO.clone()
+    Q[t, :, ::5], Q[t, :, 1::5] = torch.nan, torch.inf
+    dO[t, :, 2::3] = -torch.inf
+    c.d["Q"], c.d["dO"] = Q.to(DEV), dO.to(DEV)
+    O3, l3 = c.fwd(out_dtype=F32, want_lse=True)
+    behind = torch.ones(c.T, dtype=torch.bool)
+    behind[:t + 1] = False
+    own = torch.arange(c.T) != t
+    _, dK, dV = c.bwd(O3, l3, out_dtype=F32)
+    rg, bars = ref.backward(law, q, c.types, c.cu, c.dO, c.Q, c.K, c.V, torch.where(own[:, None, None], O3.cpu(), O.cpu()),
+                            torch.where(own[None, :], l3.cpu(), lse.cpu()))
+    assert ref.off(dK[behind.to(DEV)], rg[1][behind], bars[1][behind], False) <= 1
+    assert ref.off(dV[behind.to(DEV)], rg[2][behind], bars[2][behind], False) <= 1
