@@ -458,41 +458,62 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_k
   }
 }
 
-template <int DH, int NQ, int BQ, int NK, int BK>
-hipError_t launch_as(const AttnBwdParams& p, hipStream_t stream) {
-  static std::atomic<unsigned long long> set_q{0}, set_k{0};
-  const auto dq = attn_dq_kernel<DH, NQ, BQ>;
-  const auto dkv = attn_dkv_kernel<DH, NK, BK>;
-  constexpr int smem = ring_bytes<DH>();
-  hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(dq), set_q, NQ * smem);
+template <int DH, int NG, int NB>
+hipError_t launch_dq(const AttnBwdParams& p, hipStream_t stream) {
+  static std::atomic<unsigned long long> set{0};
+  const auto fn = attn_dq_kernel<DH, NG, NB>;
+  constexpr int smem = NG * ring_bytes<DH>();
+  const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(fn), set, smem);
   if (e != hipSuccess) return e;
-  e = ensure_lds_limit(reinterpret_cast<const void*>(dkv), set_k, NK * smem);
-  if (e != hipSuccess) return e;
-  const unsigned clear = static_cast<unsigned>(pack_clear_wgs(p.T));
-  hipLaunchKernelGGL(dq, dim3(p.q_wgs + clear), dim3(NQ * kItemThreads), NQ * smem, stream, p);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(dkv, dim3(p.k_wgs + clear), dim3(NK * kItemThreads), NK * smem, stream, p);
+  const unsigned grid = static_cast<unsigned>(p.q_wgs + pack_clear_wgs(p.T));
+  hipLaunchKernelGGL(fn, dim3(grid), dim3(NG * kItemThreads), smem, stream, p);
   return hipGetLastError();
+}
+
+template <int DH, int NG, int NB>
+hipError_t launch_dkv(const AttnBwdParams& p, hipStream_t stream) {
+  static std::atomic<unsigned long long> set{0};
+  const auto fn = attn_dkv_kernel<DH, NG, NB>;
+  constexpr int smem = NG * ring_bytes<DH>();
+  const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(fn), set, smem);
+  if (e != hipSuccess) return e;
+  const unsigned grid = static_cast<unsigned>(p.k_wgs + pack_clear_wgs(p.T));
+  hipLaunchKernelGGL(fn, dim3(grid), dim3(NG * kItemThreads), smem, stream, p);
+  return hipGetLastError();
+}
+
+hipError_t choose_dq(const AttnBwdParams& p, hipStream_t stream) {
+  const int m = p.head_dim / p.q;
+  switch (p.head_dim) {
+    case 64:
+      if (pack_few(p.q_wgs, p.cus, 64)) return launch_dq<64, 2, 0>(p, stream);
+      return blocks_fit<1>(p.law, p.q, m) ? launch_dq<64, 1, 1>(p, stream) : launch_dq<64, 1, 0>(p, stream);
+    case 128:
+      if (blocks_fit<2>(p.law, p.q, m)) return launch_dq<128, 1, 2>(p, stream);
+      return blocks_fit<1>(p.law, p.q, m) ? launch_dq<128, 1, 1>(p, stream) : launch_dq<128, 1, 0>(p, stream);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+// Head width 128: two groups always (the registers hold two wavefronts a SIMD
+// either way, and the longest walk is half as long), and all features (with
+// blocks of 32, 32 heads on 8, 8192 positions, q = 4: 538 us for 519, some
+// operands no longer fit the registers).
+hipError_t choose_dkv(const AttnBwdParams& p, hipStream_t stream) {
+  switch (p.head_dim) {
+    case 64:
+      if (pack_few(p.k_wgs, p.cus, 64)) return launch_dkv<64, 2, 0>(p, stream);
+      return blocks_fit<1>(p.law, p.q, 64 / p.q) ? launch_dkv<64, 1, 1>(p, stream) : launch_dkv<64, 1, 0>(p, stream);
+    case 128: return launch_dkv<128, 2, 0>(p, stream);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 }  // namespace
 
 hipError_t launch_attn_packed_bwd(const AttnBwdParams& p, hipStream_t stream) {
-  const bool few_q = pack_few(p.q_wgs, p.cus), few_k = pack_few(p.k_wgs, p.cus);
-  const int m = p.head_dim / p.q;
-  switch (p.head_dim) {
-    case 64:
-      if (few_q || few_k) return few_q ? launch_as<64, 2, 0, 2, 0>(p, stream) : launch_as<64, 1, 0, 2, 0>(p, stream);
-      return blocks_fit<1>(p.law, p.q, m) ? launch_as<64, 1, 1, 1, 1>(p, stream) : launch_as<64, 1, 0, 1, 0>(p, stream);
-    case 128:
-      // dK and dV: two groups always (the registers hold two wavefronts of
-      // them a SIMD either way, and the longest walk is half as long)
-      if (few_q) return launch_as<128, 2, 0, 2, 0>(p, stream);
-      if (blocks_fit<2>(p.law, p.q, m)) return launch_as<128, 1, 2, 2, 2>(p, stream);
-      return blocks_fit<1>(p.law, p.q, m) ? launch_as<128, 1, 1, 2, 1>(p, stream) : launch_as<128, 1, 0, 2, 0>(p, stream);
-    default: return hipErrorInvalidValue;
-  }
+  const hipError_t e = choose_dq(p, stream);
+  return e != hipSuccess ? e : choose_dkv(p, stream);
 }
 
 }  // namespace starq

@@ -567,7 +567,10 @@ hipError_t launch_dh(const AttnPagedParams& p, hipStream_t stream) {
 
 int32_t paged_waves(int cus) { return 2 * kWaves * cus; }
 
-// (up to 16 tiles: one sequence of 12 heads at 347 of 2048 positions FILL)
+// A whole pair to a workgroup: 16 tiles a wavefront at most.  us so, and split
+// (two launches), 12 heads of 64 in bf16: one sequence at 347 positions 7.2 and
+// 8.7 + 5.4, at 2000 16.5 and 8.8 + 6.1, at 4000 28.9 and 9.2 + 6.2; 64
+// sequences at 1000 31.4 and 32.9 + 5.2, at 2000 70.5 and 72.2 + 5.7.
 bool paged_splits(int32_t cap) { return cap > 64 * kTile; }
 
 hipError_t launch_attn_decode_paged(const AttnPagedParams& p, hipStream_t stream) {

@@ -375,8 +375,18 @@ inline int64_t pack_main_wgs(int32_t heads, int32_t max_items) {
 }
 constexpr int32_t kPackClearRows = 256;
 // Few work items (an upper bound of them) for the chip: two groups of
-// wavefronts then share a walk.
-inline bool pack_few(int64_t main_wgs, int32_t cus) { return main_wgs <= 2 * static_cast<int64_t>(cus); }
+// wavefronts then share a walk.  12 heads of 64, star law, five sequences,
+// forward, dQ, dK and dV in us with two groups and with one:
+//    500 tokens,  268 items:  12.1  14.8  14.0    13.3  15.7  16.0
+//   1500          360         17.0  22.1  22.0    20.0  23.7  27.0
+//   4000          600         30.2  38.6  50.3    37.6  46.5  54.9
+//   8000          960         65.0  85.4 114.7    63.4  80.7  97.5
+// With heads of 128 two groups fill a CU's LDS: 32 heads on 8, 500 tokens, 192
+// items: 15.6 and 23.5 (forward, dQ) for 15.4 and 21.3; 1500 tokens: 31.5 and
+// 50.2 for 29.2 and 41.8.
+inline bool pack_few(int64_t main_wgs, int32_t cus, int32_t head_dim) {
+  return head_dim == 64 && main_wgs <= 3 * static_cast<int64_t>(cus);
+}
 inline int64_t pack_clear_wgs(int32_t T) { return (T + kPackClearRows - 1) / kPackClearRows; }
 
 // Keys per decode split for a shape (a multiple of the 4 keys per team of

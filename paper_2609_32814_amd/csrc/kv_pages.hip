@@ -151,8 +151,10 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(const KvPages kv, con
   });
 }
 
-// 16 tokens a workgroup; 4 where that would leave CUs without one (64 tokens of
-// 12 heads of 64 to int8 and back: FILL)
+// 16 tokens a workgroup; 4 where that would leave CUs without one.  To int8, 64
+// sequences, 12 heads of 64, us with 4 and with 16: 64 tokens 3.8 and 4.8, 2048
+// tokens 4.8 and 5.3, 4096 6.2 and 6.1, 8192 10.8 and 9.2 (and back 3.7 and
+// 4.4, 5.4 and 5.6, 7.5 and 7.2, 11.6 and 10.0).
 constexpr int kMany = 16, kFew = 4;
 bool few_tokens(int32_t T) { return T < 256 * kMany; }
 

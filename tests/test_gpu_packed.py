@@ -94,12 +94,12 @@ CASES = [
     ("star", 4, 64, 3, 1, [1025], "random"),
     # many heads: one group of wavefronts per work item, and the star law's
     # kernels that leave feature blocks out
-    ("dense", 1, 64, 72, 72, [200, 77], None),
-    ("tensor2", 4, 64, 72, 72, [330], "interval"),
-    ("star", 2, 64, 72, 72, [150, 1], "random"),
-    ("star", 4, 64, 72, 72, [150, 99], "random"),
-    ("star", 8, 64, 72, 72, [190], "random"),
-    ("star", 4, 64, 72, 8, [170, 40], None),
+    ("dense", 1, 64, 224, 224, [200, 77], None),
+    ("tensor2", 4, 64, 144, 144, [330], "interval"),
+    ("star", 2, 64, 160, 160, [150, 1], "random"),
+    ("star", 4, 64, 96, 96, [150, 99], "random"),
+    ("star", 8, 64, 96, 96, [190], "random"),
+    ("star", 4, 64, 192, 96, [170, 40], None),
     ("dense", 1, 128, 64, 64, [140, 70], None),
     ("star", 2, 128, 64, 16, [200, 33], None),
     ("star", 4, 128, 64, 64, [150, 130], "random"),
@@ -270,7 +270,7 @@ ODD = [
     ("dense", 1, 64, 2, 2, [150, 70], None),
     ("star", 4, 64, 2, 1, [200, 30], "random"),
     ("tensor2", 2, 128, 4, 2, [140, 31], None),
-    ("star", 4, 64, 72, 72, [160, 40], None),
+    ("star", 4, 64, 96, 96, [160, 40], None),
     ("star", 4, 128, 64, 16, [170], "random"),
     ("dense", 1, 128, 64, 64, [140], None),
     ("star", 2, 64, 6, 2, [131], "some_bad"),
