@@ -62,7 +62,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 // ---- work items of a pack (see PackView) --------------------------------------
 
 __device__ __forceinline__ bool pack_matches(const PackView& v, int32_t T, int32_t n_seq, int32_t q) {
-  return v.head[0] == kPackMagic && v.head[1] == T && v.head[2] == n_seq && v.head[3] == q;
+  const int4 h = *reinterpret_cast<const int4*>(v.head);  // (one load)
+  return (h.x == kPackMagic) & (h.y == T) & (h.z == n_seq) & (h.w == q);
 }
 
 // This workgroup's head and record (see PackGrid); false: none.
