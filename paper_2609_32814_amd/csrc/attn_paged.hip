@@ -26,6 +26,12 @@
 // into its probability.  A cell of 8 features that a key's type does not
 // select, a key behind the sequence's end, of a type out of range or in a page
 // out of range is not read, and zeros stand in its place.
+//
+// Measured: 3 sequences of 250007 positions in all, 8-bit, heads of 128: 106 +
+// 9 us, 4.8 TB/s of the keys and values (a large copy reaches 5.1).  64 sequences
+// of 131072 in all, e4m3, 32 heads of 128 on 8, star law, q = 4: 56 + 8 us; 38
+// would read the selected features alone, 52 whole 128-byte lines.  One sequence at 347 positions: 7.2 us, a
+// launch and three dependent reads (page, row, output).
 #include <type_traits>
 
 #include "kv_common.hpp"
