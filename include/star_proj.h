@@ -596,7 +596,7 @@ star_status star_attn_decode(const star_attn_shape *shape, const int32_t *pos_ty
  *   (shape) bytes.
  * Errors as star_attn_fwd; STAR_ERR_WORKSPACE for a pack or ws that is too
  * small; more than STAR_PACK_MAX_SEQS sequences, or 2^32 and more chunks of 8
- * values in Q (T n_heads head_dim / 8): STAR_ERR_SHAPE.  A NaN or an infinity
+ * values in Q (T n_heads head_dim / 8), 2^24 in a row of it: STAR_ERR_SHAPE.  A NaN or an infinity
  * reaches the results that have its row among their keys (or queries), and no
  * other: not the earlier positions, not other sequences.  Workgroups that meet
  * one do their work a second time.

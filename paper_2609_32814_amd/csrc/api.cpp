@@ -1718,6 +1718,12 @@ star_status pack_layout(int32_t q, int64_t T, int32_t n_seq, PackWs& w) {
   w.end = w.key_k + keys;
   return STAR_OK;
 }
+// row offsets within a pack are counted in 32 bits of 16 bytes, the product of
+// a position and a row's width, of 24 bits each
+bool pack_fits(const AttnShape& a) {
+  const int64_t row = static_cast<int64_t>(a.H) * a.D / 8;
+  return row <= 0xffffff && a.S * row <= 0xffffffffll;
+}
 PackView pack_view(const void* buf, const PackWs& w) {
   void* p = const_cast<void*>(buf);
   return {at<int32_t>(p, 0),        at<int32_t>(p, w.perm),  at<uint8_t>(p, w.mark),
@@ -1812,8 +1818,7 @@ star_status star_attn_packed_fwd(const star_attn_shape* shape, const void* pack,
   if (!pack || pack_bytes < w.end) return STAR_ERR_WORKSPACE;
   if (!aligned16(pack) || !aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O)) return STAR_ERR_ALIGN;
   if (lse && !aligned4(lse)) return STAR_ERR_ALIGN;
-  // row offsets within a pack are counted in 32 bits of 16 bytes
-  if (static_cast<int64_t>(a.S) * a.H * a.D / 8 > 0xffffffffll) return STAR_ERR_SHAPE;
+  if (!pack_fits(a)) return STAR_ERR_SHAPE;
   const int64_t wgs = pack_main_wgs(a.H, w.max_items);
   if (wgs + pack_clear_wgs(a.S) > 0x7fffff) return STAR_ERR_SHAPE;
   AttnParams p = attn_params(a);
@@ -1854,8 +1859,7 @@ star_status star_attn_packed_bwd(const star_attn_shape* shape, const void* pack,
                         static_cast<const void*>(dV), static_cast<const void*>(ws)})
     if (!aligned16(v)) return STAR_ERR_ALIGN;
   if (!aligned4(lse)) return STAR_ERR_ALIGN;
-  // row offsets within a pack are counted in 32 bits of 16 bytes
-  if (static_cast<int64_t>(a.S) * a.H * a.D / 8 > 0xffffffffll) return STAR_ERR_SHAPE;
+  if (!pack_fits(a)) return STAR_ERR_SHAPE;
   const int64_t q_wgs = pack_main_wgs(a.H, w.max_items), k_wgs = pack_main_wgs(a.Hkv, w.max_items);
   if (q_wgs + pack_clear_wgs(a.S) > 0x7fffff) return STAR_ERR_SHAPE;
   AttnBwdParams p{};

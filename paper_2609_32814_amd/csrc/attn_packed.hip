@@ -222,15 +222,14 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 2 ? 2 : DH == 64 ? 4 : 3) 
     if (!join_groups<NCH>(acc, rings, g, wave, lane)) return;
   }
   if (my >= 0) {
-    const float inv = run_sum > 0.f ? 1.f / run_sum : 0.f;
+    const float inv = 1.f / run_sum;  // (a query is its own key: no sum is empty)
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[c][e] *= inv;
     store_row<DH>(p.O, p.odtype, qrow, acc, lh);
     if (p.lse && lh == 0)
-      p.lse[static_cast<int64_t>(h) * p.S + seq0 + my] =
-          run_sum > 0.f ? (run_max + __log2f(run_sum)) * 0.6931471805599453f : -INFINITY;
+      p.lse[static_cast<int64_t>(h) * p.S + seq0 + my] = (run_max + __log2f(run_sum)) * 0.6931471805599453f;
   }
 }
 

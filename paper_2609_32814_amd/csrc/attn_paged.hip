@@ -386,7 +386,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_split_kernel(const Att
     const int nh = min(kPagedHeads, rep - pair % p.groups * kPagedHeads);
     if (l16 < nh) {
       if (tile == 0 && t_end == n_tiles) {
-        const float inv = st.run_max == -INFINITY ? 0.f : 1.f / st.run_sum;
+        const float inv = st.run_sum == 0.f ? 0.f : 1.f / st.run_sum;
         const int64_t at = (static_cast<int64_t>(b) * p.n_heads + h0 + l16) * DH;
 #pragma unroll
         for (int e = 0; e < F; ++e)
@@ -456,14 +456,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_whole_kernel(const Att
     const float* s = wsm + x / DH * LD;
     float mx = -INFINITY;
     for (int w = 0; w < waves; ++w) mx = fmaxf(mx, s[w * kPagedHeads * LD + DH]);
+    const float base = mx == -INFINITY ? 0.f : mx;  // (no key, or scores that are no numbers, which a sum then is)
     float o = 0.f, l = 0.f;
-    if (mx != -INFINITY)
-      for (int w = 0; w < waves; ++w) {
-        const float c = __builtin_amdgcn_exp2f(s[w * kPagedHeads * LD + DH] - mx);
-        o += c * s[w * kPagedHeads * LD + x % DH];
-        l += c * s[w * kPagedHeads * LD + DH + 1];
-      }
-    store_out(p.O, p.odtype, at + x, mx == -INFINITY ? 0.f : o / l);
+    for (int w = 0; w < waves; ++w) {
+      const float c = __builtin_amdgcn_exp2f(s[w * kPagedHeads * LD + DH] - base);
+      o += c * s[w * kPagedHeads * LD + x % DH];
+      l += c * s[w * kPagedHeads * LD + DH + 1];
+    }
+    store_out(p.O, p.odtype, at + x, l == 0.f ? 0.f : o / l);
   }
 }
 
@@ -535,7 +535,7 @@ __global__ __launch_bounds__(THREADS) void attn_paged_join_kernel(const AttnPage
   float num = 0.f, den = 0.f;
   for (int x = 0; x < G; ++x) num += st[x][f];
   for (int w = 0; w < W; ++w) den += red_f[1][w];
-  store_out(p.O, p.odtype, at, mx == -INFINITY ? 0.f : num / den);
+  store_out(p.O, p.odtype, at, den == 0.f ? 0.f : num / den);
 }
 
 template <int DH, int TYPE>

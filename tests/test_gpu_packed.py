@@ -334,3 +334,21 @@ def test_what_is_not_finite_stays_out_of_masked_places(P, law, q, D, H, Hkv, len
                             torch.where(own[None, :], l3.cpu(), lse.cpu()))
     assert ref.off(dK[behind.to(DEV)], rg[1][behind], bars[1][behind], False) <= 1
     assert ref.off(dV[behind.to(DEV)], rg[2][behind], bars[2][behind], False) <= 1
+
+
+def test_a_query_that_is_no_number(P):
+    """A row of Q with a NaN, or with infinities on both sides of a product:
+    NaN in its own row of O and lse alone."""
+    for D, H in ((64, 2), (64, 96), (128, 3)):
+        c = Pack(P, "dense", 1, D, H, H, [70, 150], seed=2)
+        O, lse = c.fwd(out_dtype=F32, want_lse=True)
+        Q = c.Q.clone()
+        Q[3, :, 5] = torch.nan
+        Q[100, :, 0], Q[100, :, 1] = torch.inf, -torch.inf
+        c.d["Q"] = Q.to(DEV)
+        O1, l1 = c.fwd(out_dtype=F32, want_lse=True)
+        odd = torch.zeros(c.T, dtype=torch.bool, device=DEV)
+        odd[3] = odd[100] = True
+        assert bool(torch.isnan(O1[3]).all()) and bool(torch.isnan(l1[:, 3]).all())
+        assert not bool(torch.isfinite(O1[100]).any()) and not bool(torch.isfinite(l1[:, 100]).any())
+        assert torch.equal(O1[~odd], O[~odd]) and torch.equal(l1[:, ~odd], lse[:, ~odd])

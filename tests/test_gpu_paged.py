@@ -391,3 +391,23 @@ def test_prompts_then_steps_in_a_graph(P):
         _, _, mag = ref.forward("star", q, torch.cat([types[:n] for n in ls]), cu, *(pick(k, ls).cpu() for k in ("Q", "K", "V")))
         bar = 2 * (ref.HALF + ref.SLACK) * torch.stack([mag[z - 1] for z in cu[1:]])
         assert ref.off(out, last.cpu(), bar, False) <= 1
+
+
+@pytest.mark.parametrize("cap", [64, 4096])  # a workgroup a pair, and shares that are joined
+@pytest.mark.parametrize("kv", ["bf16", "int8"])
+def test_a_query_that_is_no_number(P, kv, cap):
+    D, H, Hkv, page, lens = 64, 4, 2, 16, [50, 64, 1] if cap == 64 else [50, 3000, 1]
+    c = Cache(P, kv, Hkv, D, page, 3, cap // page)
+    cu = [0]
+    for n in lens:
+        cu.append(cu[-1] + n)
+    P.star_kv_append(c.pages, i32(cu), i32(lens), rnd((cu[-1], Hkv, D), 1).to(DEV), rnd((cu[-1], Hkv, D), 2).to(DEV))
+    Q, t, shape = rnd((3, H, D), 3), ref.cyclic(cap, 4).to(DEV), P.AttnShape(3, cap, H, Hkv, D, 4)
+    O = P.star_attn_decode_paged(shape, c.pages, t, i32(lens), Q.to(DEV))
+    for b in range(3):
+        Qb = Q.clone()
+        Qb[b, 1] = torch.nan
+        Ob = P.star_attn_decode_paged(shape, c.pages, t, i32(lens), Qb.to(DEV))
+        odd = torch.zeros((3, H), dtype=torch.bool, device=DEV)
+        odd[b, 1] = True
+        assert bool(torch.isnan(Ob[odd]).all()) and torch.equal(Ob[~odd], O[~odd])

@@ -77,6 +77,7 @@ def test_packed_refusals(P, E):
         assert call(P, shape(P, seq_len=(1 << 18) + 1)) == E["STAR_ERR_SHAPE"]
         assert call(P, shape(P, batch=(1 << 14) + 1)) == E["STAR_ERR_SHAPE"]
         assert call(P, shape(P, batch=-1)) == E["STAR_ERR_SHAPE"]
+        assert call(P, shape(P, seq_len=2, n_heads=1 << 21, n_kv_heads=1 << 21)) == E["STAR_ERR_SHAPE"]  # a row of Q
         assert call(P, shape(P), dt=0) == E["STAR_ERR_DTYPE"]
         assert call(P, shape(P), ot=7) == E["STAR_ERR_DTYPE"]
         assert call(P, shape(P), ptr=None) == E["STAR_ERR_ARG"]
