@@ -20,7 +20,7 @@
 // is won (269 us for 266, 24576 tokens, 12 heads of 64, q = 4).
 // Measured: one sequence of 8192, all features, 64 heads of 64 in 641 us (858
 // TFLOP/s), 32 of 128 in 560 (982); the exponentials, conversions and sums of
-// 16 scores a lane (about 120 vector instructions a step) bound the first, the
+// 16 scores a lane (105 vector instructions a step, the VALU busy 71 % of the time) bound the first, the
 // products the second.  24576 tokens in 17 sequences, 12 heads of 64, star law,
 // q = 4: 221 to 250 us, by the masked halves of short walks and by the scores'
 // vector work (the law leaves products out, no exponential).  211 tokens in 3
