@@ -903,8 +903,9 @@ def star_attn_packed_fwd(shape: AttnShape, pack: torch.Tensor, Q: torch.Tensor, 
     ``shape.seq_len`` rows, Q [T, n_heads, d_h], K and V [T, n_kv_heads, d_h],
     bf16; ``pack`` from ``star_attn_pack``.  Returns O (and the log-sum-exp
     [n_heads, T] when ``want_lse`` or ``lse`` is given).  Rows outside every
-    sequence are left as they were in buffers of the caller's and are zeros
-    when this call allocates O."""
+    sequence are left as they were when the caller gives O, and are zeros (lse:
+    -infinity) when this call allocates it; an lse allocated here is -infinity
+    there."""
     T, H, Hkv, D = shape.seq_len, shape.n_heads, shape.n_kv_heads, shape.head_dim
     dev = Q.device if isinstance(Q, torch.Tensor) else None
     _need(Q, "Q", (T, H, D), _BF16, dev)
@@ -919,6 +920,8 @@ def star_attn_packed_fwd(shape: AttnShape, pack: torch.Tensor, Q: torch.Tensor, 
         _need(lse, "lse", (H, T), _F32, dev)
     elif want_lse:
         lse = torch.empty((H, T), dtype=torch.float32, device=dev)
+        if not clear:
+            lse.fill_(float("-inf"))
     _gpu(dev)
     _check(LIB.star_attn_packed_fwd(shape.ref, _ptr(pack), pack.numel(), _ptr(Q), _ptr(K), _ptr(V),
                                     DTYPES[torch.bfloat16], _ptr(O), _dt(O), _ptr(lse), int(clear), _stream(dev)),

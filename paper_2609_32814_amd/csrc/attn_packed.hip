@@ -9,8 +9,9 @@
 //       lane ends with 16 keys of one query;
 //   the causal mask where a key may lie behind a query, the running maximum
 //       and sum (fp32, base 2; a lane shares its query with lane l ^ 32);
-//   O^T += V^T P^T: P^T rounded to bf16 as it lies in the registers, V^T by
-//       transposing reads.
+//   O^T += V^T P^T: P^T rounded to bf16 as it lies in the registers (the
+//       products take no wider operand; 2^-8 of each term), V^T by transposing
+//       reads.
 // NG groups of wavefronts share the steps of one walk where there are few
 // work items; their states meet at the end.
 //
@@ -20,12 +21,11 @@
 // is won (269 us for 266, 24576 tokens, 12 heads of 64, q = 4).
 // Measured: one sequence of 8192, all features, 64 heads of 64 in 641 us (858
 // TFLOP/s), 32 of 128 in 560 (982); the exponentials, conversions and sums of
-// 16 scores a lane (105 vector instructions a step, the VALU busy 71 % of the time) bound the first, the
-// products the second.  24576 tokens in 17 sequences, 12 heads of 64, star law,
-// q = 4: 221 to 250 us, by the masked halves of short walks and by the scores'
-// vector work (the law leaves products out, no exponential).  211 tokens in 3
-// sequences: 10 us, a launch and a chain of dependent reads (plan, record,
-// positions, rows), not bytes.
+// 16 scores a lane bound the first (105 vector instructions a step, the VALU
+// busy 71 % of the time), the products the second.  24576 tokens in 17
+// sequences, 12 heads of 64, star law, q = 4: 221 to 250 us, by the same vector
+// work beside fewer products.  211 tokens in 3 sequences: 10 us, a launch and a
+// chain of dependent reads (plan, record, positions, rows), not bytes.
 #include <cfloat>
 #include <type_traits>
 

@@ -280,6 +280,7 @@ __device__ __forceinline__ Piece<DH> run_piece(const AttnPagedParams& p, int32_t
       if constexpr (TYPE != kKvBf16) pe[e] = r.scale[e] != 0.f ? pe[e] * kv_scale(r.vs[e / 4], e % 4) : 0.f;
     }
     st.run_sum += sum;  // of this lane's keys; joined at the end
+    // P in bf16: the products take no wider operand (2^-8 of each term; the sum above is of the unrounded)
     const uint4 pf = make_uint4(pack_bf16(pe[0], pe[1]), pack_bf16(pe[2], pe[3]), pack_bf16(pe[4], pe[5]), pack_bf16(pe[6], pe[7]));
     uint32_t v[8][F / 2];  // the values in bf16
 #pragma unroll

@@ -352,3 +352,17 @@ def test_a_query_that_is_no_number(P):
         assert bool(torch.isnan(O1[3]).all()) and bool(torch.isnan(l1[:, 3]).all())
         assert not bool(torch.isfinite(O1[100]).any()) and not bool(torch.isfinite(l1[:, 100]).any())
         assert torch.equal(O1[~odd], O[~odd]) and torch.equal(l1[:, ~odd], lse[:, ~odd])
+
+
+def test_lse_of_rows_outside_every_sequence(P):
+    c = Pack(P, "star", 2, 64, 2, 2, [40, 9], seed=3, tail=300, first=5)
+    rest = torch.ones(c.T, dtype=torch.bool, device=DEV)
+    rest[5:54] = False
+    O = torch.full((c.T, 2, 64), 7.0, device=DEV)
+    _, lse = c.fwd(O=O, want_lse=True)
+    assert bool(torch.isneginf(lse[:, rest]).all()) and bool(torch.isfinite(lse[:, ~rest]).all()) and bool((O[rest] == 7).all())
+    own = torch.full((2, c.T), 3.0, device=DEV)
+    c.fwd(O=O, lse=own)
+    assert bool((own[:, rest] == 3).all()) and torch.equal(own[:, ~rest], lse[:, ~rest])
+    O2, lse2 = c.fwd(lse=own, out_dtype=F32)
+    assert not O2[rest].any() and bool(torch.isneginf(lse2[:, rest]).all()) and torch.equal(O2[~rest], O[~rest])
