@@ -593,13 +593,13 @@ star_status star_attn_decode(const star_attn_shape *shape, const int32_t *pos_ty
  *   dQ [T][n_heads][head_dim], dK and dV [T][n_kv_heads][head_dim] of dtype
  *   gt.  P and dS enter their products rounded to bf16, sums are fp32, every
  *   element has one order of summation.  ws: star_attn_packed_bwd_workspace_bytes
- *   (shape) bytes.
+ *   (shape) bytes (more on a device with more compute units).
  * Errors as star_attn_fwd; STAR_ERR_WORKSPACE for a pack or ws that is too
  * small; more than STAR_PACK_MAX_SEQS sequences, or 2^32 and more chunks of 8
- * values in Q (T n_heads head_dim / 8), 2^24 in a row of it: STAR_ERR_SHAPE.  A NaN or an infinity
- * reaches the results that have its row among their keys (or queries), and no
- * other: not the earlier positions, not other sequences.  Workgroups that meet
- * one do their work a second time.
+ * values in Q (T n_heads head_dim / 8), 2^24 in a row of it: STAR_ERR_SHAPE.
+ * A NaN or an infinity reaches the results that have its row among their keys
+ * (or queries), and no other: not the earlier positions, not other sequences.
+ * Workgroups that meet one do their work a second time.
  */
 #define STAR_PACK_MAX_TOKENS (1 << 18)
 #define STAR_PACK_MAX_SEQS (1 << 14)

@@ -1835,10 +1835,32 @@ star_status star_attn_packed_fwd(const star_attn_shape* shape, const void* pack,
   return hip_status(launch_attn_packed_fwd(p, stream));
 }
 
+extern "C++" {
+namespace {
+size_t bwd_side_bytes(const AttnShape& a) { return align_up(2 * sizeof(float) * a.H * static_cast<size_t>(a.S)); }
+// Items of dK and dV walk the queries of all heads of their key/value head in
+// turn.  Where that leaves few of them for the chip, the heads are dealt to two,
+// four, ... items, whose sums a third launch adds.  dK and dV of three
+// sequences, us without and with (the sum behind the plus), and the items with:
+//   8 heads of 64 on 1    1500 tokens 125 / 27 + 4 (112)    4000 306 / 52 + 5 (272)
+//   12 of 64 on 2, q = 4  1500 tokens 107 / 60 + 5 (96)     8000 469 / 245 + 6 (296)
+//   32 of 128 on 8        1500 tokens  99 / 47 + 10 (448)   4000 242 / 149 + 14 (544)
+//                         8000 tokens 517 / 501 + 26 (1040: not taken)
+int32_t bwd_parts(const AttnShape& a, const PackWs& w) {
+  const int32_t rep = a.H / a.Hkv;
+  int32_t parts = 1;
+  while (rep % (2 * parts) == 0 && pack_main_wgs(a.Hkv * 2 * parts, w.max_items) <= 3 * static_cast<int64_t>(cu_count())) parts *= 2;
+  return parts;
+}
+}  // namespace
+}  // extern "C++"
+
 size_t star_attn_packed_bwd_workspace_bytes(const star_attn_shape* shape) {
   AttnShape a;
-  if (parse_attn(shape, a) != STAR_OK || a.S > kPackMaxTokens) return 0;
-  return align_up(2 * sizeof(float) * a.H * static_cast<size_t>(a.S));
+  PackWs w;
+  if (parse_attn(shape, a) != STAR_OK || pack_layout(a.q, a.S, a.B, w) != STAR_OK) return 0;
+  const size_t parts = static_cast<size_t>(bwd_parts(a, w));
+  return bwd_side_bytes(a) + (parts > 1 ? align_up(2 * parts * sizeof(float) * a.S * a.Hkv * a.D) : 0);
 }
 
 star_status star_attn_packed_bwd(const star_attn_shape* shape, const void* pack, size_t pack_bytes, const void* dO,
@@ -1860,7 +1882,8 @@ star_status star_attn_packed_bwd(const star_attn_shape* shape, const void* pack,
     if (!aligned16(v)) return STAR_ERR_ALIGN;
   if (!aligned4(lse)) return STAR_ERR_ALIGN;
   if (!pack_fits(a)) return STAR_ERR_SHAPE;
-  const int64_t q_wgs = pack_main_wgs(a.H, w.max_items), k_wgs = pack_main_wgs(a.Hkv, w.max_items);
+  const int32_t parts = bwd_parts(a, w);
+  const int64_t q_wgs = pack_main_wgs(a.H, w.max_items), k_wgs = pack_main_wgs(a.Hkv * parts, w.max_items);
   if (q_wgs + pack_clear_wgs(a.S) > 0x7fffff) return STAR_ERR_SHAPE;
   AttnBwdParams p{};
   p.dO = dO;
@@ -1870,6 +1893,8 @@ star_status star_attn_packed_bwd(const star_attn_shape* shape, const void* pack,
   p.O = O;
   p.lse = lse;
   p.side = static_cast<float*>(ws);
+  p.parts = parts;
+  p.part = at<float>(ws, bwd_side_bytes(a));
   p.dQ = dQ;
   p.dK = dK;
   p.dV = dV;

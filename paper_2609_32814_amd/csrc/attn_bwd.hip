@@ -19,7 +19,8 @@
 // and walks the queries from its first key on, for every query head of its
 // key/value head in turn: S = Q K^T and dP = dO V^T with the rows of Q and dO
 // from LDS and those of K and V in registers, dV^T += dO^T P and
-// dK^T += Q^T dS.
+// dK^T += Q^T dS.  With few keys the heads are dealt to several workgroups, and
+// attn_dkv_join_kernel adds their fp32 sums.
 //
 // P and dS enter their products rounded to bf16 (at most 2^-8 of each term,
 // like the operands themselves); everything else is fp32.
@@ -255,18 +256,19 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_k
     pack_clear_rows(p.pack, p.T, blockIdx.x - p.k_wgs, p.clear_rest, p.dV, p.gdtype, p.n_kv * DH);
     return;
   }
-  int hk;
+  int share;
   int32_t k;
-  if (!pack_item(p.pack, p.n_kv, hk, k)) return;
-  const int rep = p.n_heads / p.n_kv;
+  if (!pack_item(p.pack, p.n_kv * p.parts, share, k)) return;
+  // the query heads of this item: h0 .. h0 + rep - 1, of key/value head hk
+  const int hk = share / p.parts, part = share % p.parts, rep = p.n_heads / p.n_kv / p.parts, h0 = share * rep;
   const int32_t* rec = p.pack.recs_k + static_cast<int64_t>(k) * pack_rec_ints(p.q);
   const int64_t seq0 = rec[0];
   const int32_t nvalid = rec[3] >> 16;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6) % kItemWaves, g = uniform(threadIdx.x >> 6) / kItemWaves;
   const int lr = lane & 31, lh = lane >> 5;
   const int64_t ldq = static_cast<int64_t>(p.n_heads) * DH, ldk = static_cast<int64_t>(p.n_kv) * DH;
-  const uint16_t* Qg = static_cast<const uint16_t*>(p.Q) + seq0 * ldq + hk * rep * DH;
-  const uint16_t* Dg = static_cast<const uint16_t*>(p.dO) + seq0 * ldq + hk * rep * DH;
+  const uint16_t* Qg = static_cast<const uint16_t*>(p.Q) + seq0 * ldq + static_cast<int64_t>(h0) * DH;
+  const uint16_t* Dg = static_cast<const uint16_t*>(p.dO) + seq0 * ldq + static_cast<int64_t>(h0) * DH;
   const uint32_t ldq16 = static_cast<uint32_t>(ldq >> 3);
   const int row0 = wave * 32;
   const int32_t my = row0 + lr < nvalid ? p.pack.perm[rec[2] + row0 + lr] : -1;
@@ -289,7 +291,7 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_k
     side_pos = ring(step)[lr];
   };
   // rows, and by wavefront 1 their log-sum-exps and deltas
-  const float* side0 = p.side + static_cast<int64_t>(hk) * rep * p.T + seq0;
+  const float* side0 = p.side + static_cast<int64_t>(h0) * p.T + seq0;
   const float* no_side = g_attn_no_side;
   asm volatile("" : "+s"(no_side));
   auto copy = [&](int st) {
@@ -461,9 +463,32 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 1 ? 3 : 2) void attn_dkv_k
   }
   if (my >= 0) {
     const int64_t row = krow();
-    store_row<DH>(p.dK, p.gdtype, row, dk, lh, bl.own * NB / 2);
-    store_row<DH>(p.dV, p.gdtype, row, dv, lh);
+    if (p.parts == 1) {
+      store_row<DH>(p.dK, p.gdtype, row, dk, lh, bl.own * NB / 2);
+      store_row<DH>(p.dV, p.gdtype, row, dv, lh);
+    } else {
+      store_row<DH>(p.part, 0, row + part * p.T * ldk, dk, lh, bl.own * NB / 2);
+      store_row<DH>(p.part, 0, row + (p.parts + part) * p.T * ldk, dv, lh);
+    }
   }
+}
+
+// The parts of dK (blockIdx.y 0) and dV added up, in order, for the rows that
+// are tokens; four values a thread.
+__global__ __launch_bounds__(kItemThreads) void attn_dkv_join_kernel(const AttnBwdParams p) {
+  if (!pack_matches(p.pack, p.T, p.n_seq, p.q)) return;
+  const int32_t width4 = p.n_kv * p.head_dim / 4;
+  const int64_t all4 = static_cast<int64_t>(p.T) * width4, x = static_cast<int64_t>(blockIdx.x) * kItemThreads + threadIdx.x;
+  if (x >= all4 || p.pack.mark[x / width4] != 1) return;
+  const float4* from = reinterpret_cast<const float4*>(p.part) + blockIdx.y * p.parts * all4 + x;
+  float4 s = from[0];
+  for (int k = 1; k < p.parts; ++k) {
+    const float4 v = from[k * all4];
+    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+  }
+  void* out = blockIdx.y ? p.dV : p.dK;
+  if (p.gdtype == 0) static_cast<float4*>(out)[x] = s;
+  else static_cast<uint2*>(out)[x] = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
 }
 
 template <int DH, int NG, int NB>
@@ -520,8 +545,13 @@ hipError_t choose_dkv(const AttnBwdParams& p, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_attn_packed_bwd(const AttnBwdParams& p, hipStream_t stream) {
-  const hipError_t e = choose_dq(p, stream);
-  return e != hipSuccess ? e : choose_dkv(p, stream);
+  hipError_t e = choose_dq(p, stream);
+  if (e == hipSuccess) e = choose_dkv(p, stream);
+  if (e != hipSuccess || p.parts == 1) return e;
+  const int64_t threads = static_cast<int64_t>(p.T) * p.n_kv * p.head_dim / 4;
+  const unsigned grid = static_cast<unsigned>((threads + kItemThreads - 1) / kItemThreads);
+  hipLaunchKernelGGL(attn_dkv_join_kernel, dim3(grid, 2), dim3(kItemThreads), 0, stream, p);
+  return hipGetLastError();
 }
 
 }  // namespace starq

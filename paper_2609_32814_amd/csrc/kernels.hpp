@@ -351,6 +351,8 @@ struct AttnBwdParams {
   int32_t T, n_seq, n_heads, n_kv, head_dim, q, law;
   PackView pack;
   int32_t q_wgs, k_wgs;  // workgroups of the work items of either launch
+  int32_t parts;         // work items that the query heads of a key/value head are dealt to in the second
+  float* part;           // parts > 1: [2: dK, dV][parts][T][n_kv][head_dim], added up by a third launch
   int32_t cus;
   int32_t clear_rest;
 };

@@ -108,6 +108,10 @@ CASES = [
     ("star", 16, 128, 64, 64, [260], "random"),
     ("star", 4, 64, 72, 72, [140, 50, 9], "some_bad"),
     ("star", 4, 64, 2, 2, [140, 50, 9], "some_bad"),
+    # query heads of a key/value head dealt to several work items
+    ("star", 4, 64, 8, 2, [140, 50, 9], "some_bad"),
+    ("dense", 1, 128, 16, 2, [100, 0, 131], None),
+    ("tensor2", 4, 64, 12, 1, [300, 77], "interval"),
     ("dense", 1, 128, 2, 2, [100, 3], "some_bad"),
 ]
 
@@ -366,3 +370,25 @@ def test_lse_of_rows_outside_every_sequence(P):
     assert bool((own[:, rest] == 3).all()) and torch.equal(own[:, ~rest], lse[:, ~rest])
     O2, lse2 = c.fwd(lse=own, out_dtype=F32)
     assert not O2[rest].any() and bool(torch.isneginf(lse2[:, rest]).all()) and torch.equal(O2[~rest], O[~rest])
+
+
+@pytest.mark.parametrize("out_dtype", [F32, BF16])
+def test_gradient_sums_of_dealt_heads(P, out_dtype):
+    """Where heads are dealt: rows outside the sequences stay, rows of a type out
+    of range are zeros, a repeated call gives the same bits."""
+    c = Pack(P, "star", 4, 128, 8, 1, [90, 60], seed=9, tail=70, first=3, types="some_bad")
+    O, lse = c.fwd(out_dtype=F32, want_lse=True)
+    got = []
+    for _ in range(2):
+        g = [torch.full((c.T, h, 128), 7.0, dtype=out_dtype, device=DEV) for h in (8, 1, 1)]
+        c.bwd(O, lse, dQ=g[0], dK=g[1], dV=g[2])
+        got.append(g)
+    ok = ref.valid(c.types, 4)
+    inside = torch.zeros(c.T, dtype=torch.bool)
+    inside[3:153] = True
+    rg, bars = ref.backward("star", 4, c.types, c.cu, c.dO, c.Q, c.K, c.V, O.cpu(), lse.cpu())
+    for a, b, r, bar in zip(got[0], got[1], rg, bars):
+        assert torch.equal(a, b)
+        a = a.cpu()
+        assert bool((a[~inside] == 7).all()) and not a[inside & ~ok].any()
+        assert ref.off(a[inside], r[inside], bar[inside], out_dtype == BF16) <= 1
