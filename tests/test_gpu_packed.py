@@ -392,3 +392,25 @@ def test_gradient_sums_of_dealt_heads(P, out_dtype):
         a = a.cpu()
         assert bool((a[~inside] == 7).all()) and not a[inside & ~ok].any()
         assert ref.off(a[inside], r[inside], bar[inside], out_dtype == BF16) <= 1
+
+
+def test_two_streams_share_a_pack(P):
+    """Forward and gradient on two streams at once, one pack between them."""
+    a = Pack(P, "star", 4, 64, 8, 2, [300, 170, 5], seed=1)
+    b = Pack(P, "star", 4, 64, 8, 2, [300, 170, 5], seed=2)
+    want = []
+    for c in (a, b):
+        O, lse = c.fwd(want_lse=True)
+        want.append([O, lse, *c.bwd(O, lse)])
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    for _ in range(4):
+        for k, c in enumerate((a, b)):
+            with torch.cuda.stream(streams[k]):
+                c.pack = a.pack
+                O, lse = c.fwd(want_lse=True)
+                got[k].append([O, lse, *c.bwd(O, lse)])
+    torch.cuda.synchronize()
+    for k in range(2):
+        for g in got[k]:
+            assert all(torch.equal(x, y) for x, y in zip(g, want[k]))

@@ -411,3 +411,26 @@ def test_a_query_that_is_no_number(P, kv, cap):
         odd = torch.zeros((3, H), dtype=torch.bool, device=DEV)
         odd[b, 1] = True
         assert bool(torch.isnan(Ob[odd]).all()) and torch.equal(Ob[~odd], O[~odd])
+
+
+def test_two_streams_read_one_cache(P):
+    """Decode steps on two streams at once over the same pages."""
+    D, H, Hkv, page, lens, cap = 128, 8, 2, 16, [3000, 40, 900], 4096
+    c = Cache(P, "e4m3", Hkv, D, page, 3, cap // page)
+    cu = [0]
+    for n in lens:
+        cu.append(cu[-1] + n)
+    P.star_kv_append(c.pages, i32(cu), i32(lens), rnd((cu[-1], Hkv, D), 1).to(DEV), rnd((cu[-1], Hkv, D), 2).to(DEV))
+    t, length = ref.cyclic(cap, 4).to(DEV), i32(lens)
+    shape = P.AttnShape(3, cap, H, Hkv, D, 4)
+    Q = [rnd((3, H, D), 5 + k).to(DEV) for k in range(2)]
+    want = [P.star_attn_decode_paged(shape, c.pages, t, length, q) for q in Q]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    for _ in range(6):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                got[k].append(P.star_attn_decode_paged(shape, c.pages, t, length, Q[k]))
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(g, want[k]) for g in got[k])
