@@ -131,7 +131,7 @@ __global__ __launch_bounds__(NG * kItemThreads, NG == 2 ? 2 : DH == 64 ? 4 : 3) 
     after.take(ring(step + 2));
     if (now.first <= tlast) {
       const char* Kt = tiles + st * 2 * TILE;
-      if (DH == 128) tl.renew();
+      if (DH == 128) tl.renew();  // (at 64 there is room for the addresses)
       f32x16_t sc{};
       tl.template add_rows<NB>(sc, Kt, qf, bl, wx.template block<DH, NB>(bl, m));
       // keys behind a query (rows past a type's end have position kNoPos)

@@ -71,7 +71,7 @@ struct Blocks {
 };
 template <int NB>
 inline bool blocks_fit(int law, int q, int m) {
-  return NB == 0 || (law == 0 && q >= 4 && (m >= 32 ? NB == 2 : NB == 1));
+  return law == 0 && q >= 4 && (m >= 32 ? NB == 2 : NB == 1);
 }
 
 // What a work item's walk needs per type.
