@@ -639,8 +639,9 @@ star_status star_attn_packed_bwd(const star_attn_shape *shape, const void *pack,
  * V_scale 16-byte aligned (the scales are NULL for STAR_KV_BF16).
  *
  * star_kv_append writes the rows K, V (device [T][n_kv_heads][head_dim], bf16)
- * of new tokens, packed by cu_seqlens (device int32[batch + 1], as above: a
- * whole prompt, one token each, none), into the cache.  cache_len (device
+ * of new tokens, packed by cu_seqlens (device int32[batch + 1]: a whole
+ * prompt, one token each, none; bounds that cannot be count as for
+ * star_attn_pack, so one array names the same rows to both), into the cache.  cache_len (device
  * int32[batch]) is every sequence's length with them, as star_attn_decode_paged
  * then takes it: token t of sequence b is position
  * cache_len[b] - (cu_seqlens[b + 1] - t).  Tokens whose position is below 0 or
