@@ -387,12 +387,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_split_kernel(const Att
     const int nh = min(kPagedHeads, rep - pair % p.groups * kPagedHeads);
     if (l16 < nh) {
       if (tile == 0 && t_end == n_tiles) {
-        const float inv = st.run_sum == 0.f ? 0.f : 1.f / st.run_sum;
+        // (no key: zeros, also where a weight of zero has met an infinity)
+        const bool none = st.run_sum == 0.f;
+        const float inv = 1.f / st.run_sum;
         const int64_t at = (static_cast<int64_t>(b) * p.n_heads + h0 + l16) * DH;
 #pragma unroll
         for (int e = 0; e < F; ++e)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) store_out(p.O, p.odtype, at + F * (4 * quad + x) + e, st.acc[e][x] * inv);
+          for (int x = 0; x < 4; ++x) store_out(p.O, p.odtype, at + F * (4 * quad + x) + e, none ? 0.f : st.acc[e][x] * inv);
       } else {
         const int64_t slot = (static_cast<int64_t>(b) * pairs + pair + me) * slice + l16;
 #pragma unroll
