@@ -678,7 +678,9 @@ star_status star_kv_read(const star_kv_pages *pages, const int32_t *cu_seqlens,
  *   shape    batch, n_kv_heads and head_dim as in pages; seq_len the capacity
  *            max_pages * page_size
  *   pos_type device int32[seq_len]; 16-byte aligned, like every pointer
- *   cache_len, Q, O as in star_attn_decode; zero rows as there
+ *   cache_len, Q, O as in star_attn_decode; zero rows as there, and where no
+ *            cached key counts (pages that are not there).  A query whose keys
+ *            count and whose scores are all -infinity gets NaN.
  *   ws       star_attn_decode_paged_workspace_bytes(shape) bytes
  * The keys of all sequences are shared out evenly over the chip, long
  * sequences split and joined again in a second launch; the result of a call

@@ -32,6 +32,7 @@
 // of 131072 in all, e4m3, 32 heads of 128 on 8, star law, q = 4: 56 + 8 us; 38
 // would read the selected features alone, 52 whole 128-byte lines.  One sequence at 347 positions: 7.2 us, a
 // launch and three dependent reads (page, row, output).
+#include <cfloat>
 #include <type_traits>
 
 #include "kv_common.hpp"
@@ -130,6 +131,9 @@ template <int DH>
 struct Piece {
   static constexpr int F = DH / 16;
   f32x4 acc[F];  // word x of acc[e]: feature F (4 (l / 16) + x) + e of head l % 16
+  // The maximum is -infinity as long as no key has counted, and finite from then
+  // on, also where all scores are -infinity: the sum is 0 in both cases, but the
+  // result is zeros in the first and 0 / 0 in the second.
   float run_max = -INFINITY, run_sum = 0.f;
 };
 
@@ -252,7 +256,10 @@ __device__ __forceinline__ Piece<DH> run_piece(const AttnPagedParams& p, int32_t
         s[t] = mfma16(a, qf[ks], s[t]);
       }
     }
-    float sc[8], bm = -INFINITY;
+    float top = r.scale[0];  // (positive if a key counts)
+#pragma unroll
+    for (int e = 1; e < 8; ++e) top = fmaxf(top, r.scale[e]);
+    float sc[8], bm = top > 0.f ? -FLT_MAX : -INFINITY;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       float f = r.scale[e];
@@ -388,7 +395,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_split_kernel(const Att
     if (l16 < nh) {
       if (tile == 0 && t_end == n_tiles) {
         // (no key: zeros, also where a weight of zero has met an infinity)
-        const bool none = st.run_sum == 0.f;
+        const bool none = st.run_max == -INFINITY;
         const float inv = 1.f / st.run_sum;
         const int64_t at = (static_cast<int64_t>(b) * p.n_heads + h0 + l16) * DH;
 #pragma unroll
@@ -459,14 +466,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_whole_kernel(const Att
     const float* s = wsm + x / DH * LD;
     float mx = -INFINITY;
     for (int w = 0; w < waves; ++w) mx = fmaxf(mx, s[w * kPagedHeads * LD + DH]);
-    const float base = mx == -INFINITY ? 0.f : mx;  // (no key, or scores that are no numbers, which a sum then is)
+    const float base = mx == -INFINITY ? 0.f : mx;  // (no key)
     float o = 0.f, l = 0.f;
     for (int w = 0; w < waves; ++w) {
       const float c = __builtin_amdgcn_exp2f(s[w * kPagedHeads * LD + DH] - base);
       o += c * s[w * kPagedHeads * LD + x % DH];
       l += c * s[w * kPagedHeads * LD + DH + 1];
     }
-    store_out(p.O, p.odtype, at + x, l == 0.f ? 0.f : o / l);
+    store_out(p.O, p.odtype, at + x, mx == -INFINITY ? 0.f : o / l);
   }
 }
 
@@ -507,7 +514,7 @@ __global__ __launch_bounds__(THREADS) void attn_paged_join_kernel(const AttnPage
   if ((threadIdx.x & 63) == 0) red_f[0][wave] = mx;
   __syncthreads();
   for (int w = 0; w < W; ++w) mx = fmaxf(mx, red_f[0][w]);
-  const float base = mx == -INFINITY ? 0.f : mx;  // (all pieces without a key: zeros over zeros below)
+  const float base = mx == -INFINITY ? 0.f : mx;  // (all pieces without a key)
 
   float o = 0.f, l = 0.f;
   for (int32_t x0 = 0; x0 < pieces; x0 += THREADS) {
@@ -538,7 +545,7 @@ __global__ __launch_bounds__(THREADS) void attn_paged_join_kernel(const AttnPage
   float num = 0.f, den = 0.f;
   for (int x = 0; x < G; ++x) num += st[x][f];
   for (int w = 0; w < W; ++w) den += red_f[1][w];
-  store_out(p.O, p.odtype, at, den == 0.f ? 0.f : num / den);
+  store_out(p.O, p.odtype, at, mx == -INFINITY ? 0.f : num / den);
 }
 
 template <int DH, int TYPE>

@@ -1,11 +1,12 @@
-"""The paged decode step where a query has no key that counts: zeros, whatever
-the capacity and however the keys are dealt out."""
+"""The paged decode step where a query has no key that counts, and where its
+keys count and weigh nothing: zeros in the first case, the formula's 0 / 0 in
+the second, whatever the capacity and however the keys are dealt out."""
 
 import pytest
 import torch
 
 import attn_ref as ref
-from test_gpu_paged import DEV, F32, Cache, P, i32, rnd  # noqa: F401 (P: fixture)
+from test_gpu_paged import DEV, F32, Cache, P, i32, rnd, stored  # noqa: F401 (P: fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +45,49 @@ def test_query_of_no_type_over_values_that_are_not_finite(P, kv, cap, lens):
     for O in outs:
         assert not O[:2].any() and bool(torch.isfinite(O).all()) and O[2].any() and O[3].any()
     assert torch.equal(outs[0], outs[1])
+
+
+@pytest.mark.parametrize("cap", [2048, 4096])
+@pytest.mark.parametrize("kv", ["bf16", "int8"])
+@pytest.mark.parametrize("lens", [[40, 64, 30], [1500, 33, 700]])
+def test_keys_that_all_weigh_nothing(P, kv, cap, lens):
+    """Every score of one query minus infinity: its softmax is 0 / 0, no
+    number, as in the packed forward; not the zeros of a query without keys."""
+    H, Hkv, D = 4, 2, 64
+    K = [rnd((n, Hkv, D), 10 + b) for b, n in enumerate(lens)]
+    V = [rnd((n, Hkv, D), 20 + b) for b, n in enumerate(lens)]
+    for x in K:
+        x[:, :, 0] = -1.0
+    c = filled(P, kv, K, V, lens, cap)
+    Q, shape, t = rnd((3, H, D), 5), P.AttnShape(3, cap, H, Hkv, D, 1, "dense"), torch.zeros(cap, dtype=torch.int32)
+    O = P.star_attn_decode_paged(shape, c.pages, t.to(DEV), i32(lens), Q.to(DEV), out_dtype=F32)
+    for b in range(3):
+        Qb = Q.clone()
+        Qb[b, 2, 0] = torch.inf
+        Ob = P.star_attn_decode_paged(shape, c.pages, t.to(DEV), i32(lens), Qb.to(DEV), out_dtype=F32)
+        odd = torch.zeros((3, H), dtype=torch.bool, device=DEV)
+        odd[b, 2] = True
+        assert bool(torch.isnan(Ob[odd]).all()) and torch.equal(Ob[~odd], O[~odd])
+
+
+@pytest.mark.parametrize("cap", [2048, 4096])
+@pytest.mark.parametrize("first", [True, False])
+def test_keys_some_of_which_weigh_nothing(P, cap, first):
+    """Scores below the lowest finite number (3e38 times -3e38) in the first
+    or the last three quarters of the keys, whole tiles and whole shares of
+    them: these have no weight, the others theirs."""
+    H, Hkv, D, lens = 2, 1, 64, [1600, 70, 5]
+    K = [rnd((n, Hkv, D), 10 + b) for b, n in enumerate(lens)]
+    V = [rnd((n, Hkv, D), 20 + b) for b, n in enumerate(lens)]
+    for x, n in zip(K, lens):
+        x[:, :, 0] = 0
+        rows = slice(0, 3 * n // 4) if first else slice(n // 4, n)
+        x[rows, :, 0] = -3e38
+    Q = rnd((3, H, D), 5)
+    Q[:, :, 0] = 3e38
+    c = filled(P, "bf16", K, V, lens, cap)
+    t = torch.zeros(cap, dtype=torch.int32)
+    O = P.star_attn_decode_paged(P.AttnShape(3, cap, H, Hkv, D, 1, "dense"), c.pages, t.to(DEV), i32(lens), Q.to(DEV),
+                                 out_dtype=F32)
+    rO, mag = ref.decode("dense", 1, t, lens, Q, [stored("bf16", x)[0] for x in K], [stored("bf16", x)[0] for x in V])
+    assert ref.off(O, rO, (ref.HALF + ref.SLACK) * mag, False) <= 1
