@@ -980,7 +980,9 @@ class KVPages:
     page_size, d_h] of bfloat16, float8_e4m3fn or int8, page_table
     [sequences, max_pages] (int32), and for the 8-bit types the scale bytes
     K_scale and V_scale [n_pages, n_kv_heads, page_size] (uint8).  The tensors
-    stay the caller's: a page table written in place is seen by the next call."""
+    stay the caller's: a page table written in place is seen by the next call.
+    Their addresses are taken once, so another tensor takes another KVPages;
+    the attributes cannot be assigned."""
 
     def __init__(self, K_pages: torch.Tensor, V_pages: torch.Tensor, page_table: torch.Tensor, K_scale=None,
                  V_scale=None):
@@ -1007,6 +1009,11 @@ class KVPages:
                             KV_TYPES[K_pages.dtype], _ptr(K_pages), _ptr(V_pages), _ptr(K_scale), _ptr(V_scale),
                             _ptr(page_table))
         self.ref = ctypes.byref(self._c)
+
+    def __setattr__(self, name, value):
+        if "ref" in self.__dict__:  # (a tensor put aside here would be freed under the pointer that the calls take)
+            raise AttributeError(f"KVPages.{name} cannot be assigned: make another KVPages")
+        object.__setattr__(self, name, value)
 
     @property
     def capacity(self) -> int:
