@@ -8,6 +8,7 @@ this module fails loudly if ``libstarq.so`` has not been built.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Sequence
@@ -250,6 +251,16 @@ def _gpu(device):
     """Every tensor of a call sits on `device`; it must be a GPU."""
     if device.type != "cuda":
         raise ValueError("the library takes GPU tensors only")
+
+
+_SAME = contextlib.nullcontext()
+
+
+def _on(device):
+    """A context in which `device` is the current one.  The library asks the
+    current device for its compute units and raises the LDS limit there, and a
+    default stream is the current device's, whatever device it was asked for."""
+    return _SAME if torch.cuda.current_device() == device.index else torch.cuda.device(device)
 
 
 def _opt(t, name: str, shape, dtypes=None, device=None):
@@ -892,8 +903,9 @@ def star_attn_pack(q: int, row_type: torch.Tensor, cu_seqlens: torch.Tensor, pac
         pack = torch.empty(max(star_attn_pack_bytes(q, T, n), 16), dtype=torch.uint8, device=dev)
     _need(pack, "pack", (pack.numel(),), (torch.uint8,), dev)
     _gpu(dev)
-    _check(LIB.star_attn_pack(int(q), T, n, _ptr(row_type), _ptr(cu_seqlens), _ptr(pack), pack.numel(), _stream(dev)),
-           "star_attn_pack")
+    with _on(dev):
+        _check(LIB.star_attn_pack(int(q), T, n, _ptr(row_type), _ptr(cu_seqlens), _ptr(pack), pack.numel(), _stream(dev)),
+               "star_attn_pack")
     return pack
 
 
@@ -923,9 +935,10 @@ def star_attn_packed_fwd(shape: AttnShape, pack: torch.Tensor, Q: torch.Tensor, 
         if not clear:
             lse.fill_(float("-inf"))
     _gpu(dev)
-    _check(LIB.star_attn_packed_fwd(shape.ref, _ptr(pack), pack.numel(), _ptr(Q), _ptr(K), _ptr(V),
-                                    DTYPES[torch.bfloat16], _ptr(O), _dt(O), _ptr(lse), int(clear), _stream(dev)),
-           "star_attn_packed_fwd")
+    with _on(dev):
+        _check(LIB.star_attn_packed_fwd(shape.ref, _ptr(pack), pack.numel(), _ptr(Q), _ptr(K), _ptr(V),
+                                        DTYPES[torch.bfloat16], _ptr(O), _dt(O), _ptr(lse), int(clear), _stream(dev)),
+               "star_attn_packed_fwd")
     return (O, lse) if lse is not None else O
 
 
@@ -959,14 +972,15 @@ def star_attn_packed_bwd(shape: AttnShape, pack: torch.Tensor, dO: torch.Tensor,
     _need(dQ, "dQ", (T, H, D), _FLOATS, dev)
     _need(dK, "dK", (T, Hkv, D), (dQ.dtype,), dev)
     _need(dV, "dV", (T, Hkv, D), (dQ.dtype,), dev)
-    if ws is None:
-        ws = torch.empty(max(star_attn_packed_bwd_workspace_bytes(shape), 16), dtype=torch.uint8, device=dev)
-    _need(ws, "ws", tuple(ws.shape), None, dev)
     _gpu(dev)
-    _check(LIB.star_attn_packed_bwd(shape.ref, _ptr(pack), pack.numel(), _ptr(dO), _ptr(Q), _ptr(K), _ptr(V),
-                                    DTYPES[torch.bfloat16], _ptr(O), _dt(O), _ptr(lse), _ptr(dQ), _ptr(dK), _ptr(dV),
-                                    _dt(dQ), int(not any(given)), _ptr(ws), ws.numel() * ws.element_size(),
-                                    _stream(dev)), "star_attn_packed_bwd")
+    with _on(dev):
+        if ws is None:
+            ws = torch.empty(max(star_attn_packed_bwd_workspace_bytes(shape), 16), dtype=torch.uint8, device=dev)
+        _need(ws, "ws", tuple(ws.shape), None, dev)
+        _check(LIB.star_attn_packed_bwd(shape.ref, _ptr(pack), pack.numel(), _ptr(dO), _ptr(Q), _ptr(K), _ptr(V),
+                                        DTYPES[torch.bfloat16], _ptr(O), _dt(O), _ptr(lse), _ptr(dQ), _ptr(dK),
+                                        _ptr(dV), _dt(dQ), int(not any(given)), _ptr(ws),
+                                        ws.numel() * ws.element_size(), _stream(dev)), "star_attn_packed_bwd")
     return dQ, dK, dV
 
 
@@ -1042,8 +1056,9 @@ def star_kv_append(pages: KVPages, cu_seqlens: torch.Tensor, cache_len: torch.Te
     dev = _kv_rows(pages, cu_seqlens, cache_len)
     _need(K, "K", (T, pages.n_kv_heads, pages.head_dim), _BF16, dev)
     _need(V, "V", (T, pages.n_kv_heads, pages.head_dim), _BF16, dev)
-    _check(LIB.star_kv_append(pages.ref, _ptr(cu_seqlens), _ptr(cache_len), T, _ptr(K), _ptr(V),
-                              DTYPES[torch.bfloat16], _stream(dev)), "star_kv_append")
+    with _on(dev):
+        _check(LIB.star_kv_append(pages.ref, _ptr(cu_seqlens), _ptr(cache_len), T, _ptr(K), _ptr(V),
+                                  DTYPES[torch.bfloat16], _stream(dev)), "star_kv_append")
 
 
 def star_kv_read(pages: KVPages, cu_seqlens: torch.Tensor, cache_len: torch.Tensor, T: int, K=None, V=None):
@@ -1061,8 +1076,9 @@ def star_kv_read(pages: KVPages, cu_seqlens: torch.Tensor, cache_len: torch.Tens
     else:
         _need(K, "K", shape, _BF16, dev)
         _need(V, "V", shape, _BF16, dev)
-    _check(LIB.star_kv_read(pages.ref, _ptr(cu_seqlens), _ptr(cache_len), int(T), _ptr(K), _ptr(V),
-                            DTYPES[torch.bfloat16], int(clear), _stream(dev)), "star_kv_read")
+    with _on(dev):
+        _check(LIB.star_kv_read(pages.ref, _ptr(cu_seqlens), _ptr(cache_len), int(T), _ptr(K), _ptr(V),
+                                DTYPES[torch.bfloat16], int(clear), _stream(dev)), "star_kv_read")
     return K, V
 
 
@@ -1083,10 +1099,11 @@ def star_attn_decode_paged(shape: AttnShape, pages: KVPages, pos_type: torch.Ten
         O = torch.empty((B, H, D), dtype=out_dtype, device=dev)
     _need(O, "O", (B, H, D), _FLOATS, dev)
     _gpu(dev)
-    if ws is None:
-        ws = torch.empty(max(star_attn_decode_paged_workspace_bytes(shape), 16), dtype=torch.uint8, device=dev)
-    _need(ws, "ws", tuple(ws.shape), None, dev)
-    _check(LIB.star_attn_decode_paged(shape.ref, pages.ref, _ptr(pos_type), _ptr(cache_len), _ptr(Q),
-                                      DTYPES[torch.bfloat16], _ptr(O), _dt(O), _ptr(ws),
-                                      ws.numel() * ws.element_size(), _stream(dev)), "star_attn_decode_paged")
+    with _on(dev):
+        if ws is None:
+            ws = torch.empty(max(star_attn_decode_paged_workspace_bytes(shape), 16), dtype=torch.uint8, device=dev)
+        _need(ws, "ws", tuple(ws.shape), None, dev)
+        _check(LIB.star_attn_decode_paged(shape.ref, pages.ref, _ptr(pos_type), _ptr(cache_len), _ptr(Q),
+                                          DTYPES[torch.bfloat16], _ptr(O), _dt(O), _ptr(ws),
+                                          ws.numel() * ws.element_size(), _stream(dev)), "star_attn_decode_paged")
     return O
