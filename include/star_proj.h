@@ -649,7 +649,9 @@ star_status star_attn_packed_bwd(const star_attn_shape *shape, const void *pack,
  * star_kv_read is the inverse: the same arguments, K and V are written (rows
  * without an entry: zeros; rows outside every sequence: left as they were, or
  * zeros with clear_rest).
+ * More than STAR_KV_MAX_TOKENS rows in one call: STAR_ERR_SHAPE.
  */
+#define STAR_KV_MAX_TOKENS ((1 << 28) - 16)
 typedef enum { STAR_KV_BF16 = 0, STAR_KV_E4M3 = 1, STAR_KV_INT8 = 2 } star_kv_type;
 typedef struct {
     int32_t n_pages;

@@ -1695,7 +1695,8 @@ star_status star_attn_decode(const star_attn_shape* shape, const int32_t* pos_ty
 extern "C++" {
 namespace {
 
-static_assert(STAR_PACK_MAX_TOKENS == kPackMaxTokens && STAR_PACK_MAX_SEQS == kPackMaxSeqs, "one limit for the ABI and the kernels");
+static_assert(STAR_PACK_MAX_TOKENS == kPackMaxTokens && STAR_PACK_MAX_SEQS == kPackMaxSeqs && STAR_KV_MAX_TOKENS == kKvMaxTokens,
+              "one limit for the ABI and the kernels");
 
 struct PackWs {
   int32_t max_items = 0;
@@ -1758,7 +1759,7 @@ star_status check_pages(const KvPages& kv) {
 star_status check_rows(const KvPages& kv, int64_t T, const int32_t* cu, const int32_t* cache_len, const void* K,
                        const void* V, star_dtype dt) {
   if (dt != STAR_BF16) return STAR_ERR_DTYPE;
-  if (T < 0 || T > 0x7fffff00) return STAR_ERR_SHAPE;
+  if (T < 0 || T > kKvMaxTokens) return STAR_ERR_SHAPE;
   if (kv.n_kv > (1 << 20)) return STAR_ERR_SHAPE;  // 16 n_kv rows of a workgroup are counted in 32 bits
   if (T == 0) return STAR_OK;
   if (!cu || !cache_len || !K || !V) return STAR_ERR_ARG;

@@ -412,6 +412,9 @@ struct KvPages {
   int32_t n_pages, page_shift, n_kv, head_dim, B, max_pages, type;
 };
 constexpr int32_t kKvMaxCapacity = 1 << 30;  // positions per sequence
+// Rows of one append or read: a launch has less than 2^32 threads, and 16 rows
+// take 256 of them.
+constexpr int32_t kKvMaxTokens = (1 << 28) - 16;
 
 // Token t of sequence b (cu[b] <= t < cu[b + 1]) is position
 // cache_len[b] - (cu[b + 1] - t).  K, V [T][n_kv][head_dim] bf16.

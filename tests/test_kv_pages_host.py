@@ -1,5 +1,5 @@
-"""KVPages on the host: the addresses that the calls take are those of the
-tensors that it holds."""
+"""The paged cache on the host: KVPages keeps the tensors whose addresses the
+calls take; the sizes that a launch can hold."""
 
 import ctypes
 
@@ -26,3 +26,21 @@ def test_tensors_cannot_be_swapped_under_the_pointers(dtype):
         assert (got or None) == (t.data_ptr() if t is not None else None)
     table[0, 0] = 2  # in place: seen, the same memory
     assert kv.page_table[0, 0] == 2
+
+
+def test_rows_that_no_launch_holds_are_refused():
+    """2^28 rows and more would take 2^32 threads (fake pointers, never read:
+    a refusal comes first; one row fewer is refused for a pointer instead)."""
+    import paper_2609_32814_amd as P
+
+    b = P.binding
+    shape = {v: k for k, v in b.STATUS_NAMES.items()}["STAR_ERR_SHAPE"]
+    arg = {v: k for k, v in b.STATUS_NAMES.items()}["STAR_ERR_ARG"]
+    V = ctypes.c_void_p
+    pg = b._CKvPages(10, 16, 2, 64, 2, 4, 1, 16, 16, 16, 16, 16)
+    top = (1 << 28) - 16
+    for T in (top + 1, 1 << 28, 0x7fffff00, 1 << 40):
+        assert b.LIB.star_kv_append(ctypes.byref(pg), V(16), V(16), T, V(16), V(16), 1, None) == shape
+        assert b.LIB.star_kv_read(ctypes.byref(pg), V(16), V(16), T, V(16), V(16), 1, 0, None) == shape
+    assert b.LIB.star_kv_append(ctypes.byref(pg), V(16), V(16), top, None, V(16), 1, None) == arg
+    assert b.LIB.star_kv_read(ctypes.byref(pg), V(16), V(16), top, None, V(16), 1, 0, None) == arg
