@@ -1841,17 +1841,26 @@ namespace {
 size_t bwd_side_bytes(const AttnShape& a) { return align_up(2 * sizeof(float) * a.H * static_cast<size_t>(a.S)); }
 // Items of dK and dV walk the queries of all heads of their key/value head in
 // turn.  Where that leaves few of them for the chip, the heads are dealt to two,
-// four, ... items, whose sums a third launch adds.  dK and dV of three
-// sequences, us without and with (the sum behind the plus), and the items with:
-//   8 heads of 64 on 1    1500 tokens 125 / 27 + 4 (112)    4000 306 / 52 + 5 (272)
-//   12 of 64 on 2, q = 4  1500 tokens 107 / 60 + 5 (96)     8000 469 / 245 + 6 (296)
-//   32 of 128 on 8        1500 tokens  99 / 47 + 10 (448)   4000 242 / 149 + 14 (544)
-//                         8000 tokens 517 / 501 + 26 (1040: not taken)
+// four, ... items, whose sums a third launch adds.  That launch takes 4 us and
+// more, and two groups of wavefronts share a walk's steps of about 1 us: it pays
+// if it shortens the walk of a sequence of mean length by 9 steps.  dK and dV
+// of three sequences, us without and with (all launches; a type's steps are
+// rounded up), and the steps that it leaves out of a walk of mean length:
+//   2 heads of 64 a key head 200 tokens  12 / 16 (3)     400  17 / 18 (5)    800  25 / 22 (9)
+//   2 of 128                 200         18 / 21 (3)     400  25 / 25 (5)    800  36 / 32 (9)
+//   4 of 128                  50         15 / 16 (3)     100  19 / 18 (6)    200  24 / 23 (9)    1500   98 / 58
+//   8 of 64                   50         14 / 15 (7)     100  19 / 17 (14)   400  41 / 18 (35)   4000  307 / 58
+//   6 of 64, star, q = 4      20         29 / 22 (12)    400  44 / 31 (48)                       4000  242 / 133
+// And not where there are items enough: 4 of 128, 8000 tokens 517 / 527 (1040
+// items; 4000 tokens, 544 items: 237 / 170).
+constexpr int64_t kDealSteps = 9;
 int32_t bwd_parts(const AttnShape& a, const PackWs& w) {
   const int32_t rep = a.H / a.Hkv;
   int32_t parts = 1;
   while (rep % (2 * parts) == 0 && pack_main_wgs(a.Hkv * 2 * parts, w.max_items) <= 3 * static_cast<int64_t>(cu_count())) parts *= 2;
-  return parts;
+  const int64_t rows = int64_t{32} * a.q * std::max(a.B, 1);  // a step of every type of every sequence
+  const int64_t steps = a.q * ((a.S + rows - 1) / rows);      // of a walk, for one head
+  return (rep - rep / parts) * steps >= kDealSteps ? parts : 1;
 }
 }  // namespace
 }  // extern "C++"
