@@ -1932,7 +1932,7 @@ star_status star_kv_append(const star_kv_pages* pages, const int32_t* cu_seqlens
   if (st != STAR_OK) return st;
   st = check_rows(kv, T, cu_seqlens, cache_len, K, V, dt);
   if (st != STAR_OK || T == 0 || kv.B == 0) return st;
-  return hip_status(launch_kv_append(kv, cu_seqlens, cache_len, static_cast<int32_t>(T), K, V, stream));
+  return hip_status(launch_kv_append(kv, cu_seqlens, cache_len, static_cast<int32_t>(T), K, V, cu_count(), stream));
 }
 
 star_status star_kv_read(const star_kv_pages* pages, const int32_t* cu_seqlens, const int32_t* cache_len, int64_t T,
@@ -1942,7 +1942,7 @@ star_status star_kv_read(const star_kv_pages* pages, const int32_t* cu_seqlens, 
   if (st != STAR_OK) return st;
   st = check_rows(kv, T, cu_seqlens, cache_len, K, V, dt);
   if (st != STAR_OK || T == 0) return st;
-  return hip_status(launch_kv_read(kv, cu_seqlens, cache_len, static_cast<int32_t>(T), K, V, clear_rest, stream));
+  return hip_status(launch_kv_read(kv, cu_seqlens, cache_len, static_cast<int32_t>(T), K, V, clear_rest, cu_count(), stream));
 }
 
 size_t star_attn_decode_paged_workspace_bytes(const star_attn_shape* shape) {

@@ -519,7 +519,7 @@ hipError_t choose_dq(const AttnBwdParams& p, hipStream_t stream) {
   const int m = p.head_dim / p.q;
   switch (p.head_dim) {
     case 64:
-      if (pack_few(p.q_wgs, p.cus, 64)) return launch_dq<64, 2, 0>(p, stream);
+      if (pack_few(p.q_wgs, p.cus)) return launch_dq<64, 2, 0>(p, stream);
       return blocks_fit<1>(p.law, p.q, m) ? launch_dq<64, 1, 1>(p, stream) : launch_dq<64, 1, 0>(p, stream);
     case 128:
       if (blocks_fit<2>(p.law, p.q, m)) return launch_dq<128, 1, 2>(p, stream);
@@ -535,7 +535,7 @@ hipError_t choose_dq(const AttnBwdParams& p, hipStream_t stream) {
 hipError_t choose_dkv(const AttnBwdParams& p, hipStream_t stream) {
   switch (p.head_dim) {
     case 64:
-      if (pack_few(p.k_wgs, p.cus, 64)) return launch_dkv<64, 2, 0>(p, stream);
+      if (pack_few(p.k_wgs, p.cus)) return launch_dkv<64, 2, 0>(p, stream);
       return blocks_fit<1>(p.law, p.q, 64 / p.q) ? launch_dkv<64, 1, 1>(p, stream) : launch_dkv<64, 1, 0>(p, stream);
     case 128: return launch_dkv<128, 2, 0>(p, stream);
     default: return hipErrorInvalidValue;

@@ -251,7 +251,7 @@ hipError_t launch_attn_packed_fwd(const AttnParams& p, hipStream_t stream) {
   const int m = p.head_dim / p.q;
   switch (p.head_dim) {
     case 64:
-      if (pack_few(p.main_wgs, p.cus, 64)) return launch<64, 2, 0>(p, stream);
+      if (pack_few(p.main_wgs, p.cus)) return launch<64, 2, 0>(p, stream);
       return blocks_fit<1>(p.law, p.q, m) ? launch<64, 1, 1>(p, stream) : launch<64, 1, 0>(p, stream);
     case 128:
       if (blocks_fit<2>(p.law, p.q, m)) return launch<128, 1, 2>(p, stream);

@@ -12,9 +12,15 @@
 //   last position of step h + 2;
 //   compute with the tile of step h.
 // The barrier of body h says that every wavefront is through with body h - 1,
-// whose tile (h - 1) mod 3 = (h + 2) mod 3 the new copies overwrite.  All
-// memory traffic of the loop is copies into LDS, counted by hand: a body
-// leaves what the body before it asked for in flight at its wait.
+// whose tile (h - 1) mod 3 = (h + 2) mod 3 the new copies overwrite.  The
+// copies into LDS are counted by hand: a body leaves what the body before it
+// asked for in flight at its wait.  Other loads in between are safe, since a
+// wait for the same count then waits for more, but the compiler, which does
+// not see the copies, waits behind its own until nothing is in flight.  It has
+// some where the registers do not hold all: in the first walk, dQ at width 64
+// with feature blocks brings a quarter of Q's operands back from scratch in
+// steps whose type lies in the second block from the own one (8 registers), and
+// dK/dV does so in masked steps (with one group at width 64, and at 128).
 #pragma once
 
 #include "attn_common.hpp"
@@ -69,6 +75,14 @@ struct Blocks {
   // turn-th 16 features from the own block on
   __device__ __forceinline__ int turned(int ks) const { return NB > 0 ? ((own * NB) + ks) % KS : ks; }
 };
+// From four groups on (with two, every pair of unlike types keeps all features,
+// and no block of half of them is built).  us with blocks and without:
+//   24576 tokens in 17 sequences, 12 heads of 64
+//     q = 4  forward 246 / 257  dQ 331 / 330 (299 / 309)  dK and dV 398 / 418
+//     q = 8          301 / 321     348 / 362                        435 / 468
+//   8192 in 6, 32 heads of 128 on 8
+//     q = 4  forward 234 / 249  dQ 348 / 390
+//     q = 8          266 / 303     404 / 446
 template <int NB>
 inline bool blocks_fit(int law, int q, int m) {
   return law == 0 && q >= 4 && (m >= 32 ? NB == 2 : NB == 1);

@@ -256,11 +256,6 @@ hipError_t launch_decode_phase(const DecodePhase& p, hipStream_t stream);
 
 // ---- algebraic attention ------------------------------------------------------
 
-// Feature groups of width m = head_dim / q inside every head; layouts are
-// token-major: Q and O [B][S][n_heads][head_dim], K and V
-// [B][S][n_kv][head_dim] (bf16), query head h reads key/value head
-// h / (n_heads / n_kv).
-
 // The plan of a pack: n_seq sequences of different lengths, one behind the
 // other in T rows, their tokens sorted by (sequence, type, position).  A work
 // item is a block of up to kAttnBlockRows tokens of one type of one sequence.
@@ -284,9 +279,9 @@ struct PackView {
   uint8_t* mark;   // [T] 1: a token; 0: its type is out of range; 2: outside every sequence
   int32_t* recs_q;
   int32_t* recs_k;
-  int32_t* raw_q;  // the same before they are sorted, -1 in word 3 of the unused ones
+  int32_t* raw_q;  // the same before they are sorted
   int32_t* raw_k;
-  int32_t* key_q;  // what they are sorted by, per raw record
+  int32_t* key_q;  // what they are sorted by, per raw record (-1: unused)
   int32_t* key_k;
 };
 #ifdef __HIPCC__
@@ -303,6 +298,10 @@ STARQ_HD inline int32_t pack_raw_base(int64_t start, int64_t s, int64_t q) {
 hipError_t launch_attn_pack(const int32_t* types, const int32_t* cu, int32_t T, int32_t n_seq, int32_t q, const PackView& pack,
                             hipStream_t stream);
 
+// Feature groups of width m = head_dim / q inside every head; layouts are
+// token-major: Q and O [B][S][n_heads][head_dim], K and V
+// [B][S][n_kv][head_dim] (bf16), query head h reads key/value head
+// h / (n_heads / n_kv).
 struct AttnParams {
   const void* Q;
   const void* K;
@@ -383,12 +382,10 @@ constexpr int32_t kPackClearRows = 256;
 //   1500          360         17.0  22.1  22.0    20.0  23.7  27.0
 //   4000          600         30.2  38.6  50.3    37.6  46.5  54.9
 //   8000          960         65.0  85.4 114.7    63.4  80.7  97.5
-// With heads of 128 two groups fill a CU's LDS: 32 heads on 8, 500 tokens, 192
-// items: 15.6 and 23.5 (forward, dQ) for 15.4 and 21.3; 1500 tokens: 31.5 and
-// 50.2 for 29.2 and 41.8.
-inline bool pack_few(int64_t main_wgs, int32_t cus, int32_t head_dim) {
-  return head_dim == 64 && main_wgs <= 3 * static_cast<int64_t>(cus);
-}
+// Heads of 64 only: with heads of 128 two groups fill a CU's LDS, and 32 heads on
+// 8 took 15.6 and 23.5 (forward, dQ) for 15.4 and 21.3 at 500 tokens, 192 items,
+// and 31.5 and 50.2 for 29.2 and 41.8 at 1500.
+inline bool pack_few(int64_t main_wgs, int32_t cus) { return main_wgs <= 3 * static_cast<int64_t>(cus); }
 inline int64_t pack_clear_wgs(int32_t T) { return (T + kPackClearRows - 1) / kPackClearRows; }
 
 // Keys per decode split for a shape (a multiple of the 4 keys per team of
@@ -419,9 +416,9 @@ constexpr int32_t kKvMaxTokens = (1 << 28) - 16;
 // Token t of sequence b (cu[b] <= t < cu[b + 1]) is position
 // cache_len[b] - (cu[b + 1] - t).  K, V [T][n_kv][head_dim] bf16.
 hipError_t launch_kv_append(const KvPages& kv, const int32_t* cu, const int32_t* cache_len, int32_t T, const void* K,
-                            const void* V, hipStream_t stream);
+                            const void* V, int32_t cus, hipStream_t stream);
 hipError_t launch_kv_read(const KvPages& kv, const int32_t* cu, const int32_t* cache_len, int32_t T, void* K, void* V,
-                          int32_t clear_rest, hipStream_t stream);
+                          int32_t clear_rest, int32_t cus, hipStream_t stream);
 
 struct AttnPagedParams {
   KvPages kv;

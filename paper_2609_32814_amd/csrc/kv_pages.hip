@@ -196,7 +196,7 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(const KvPages kv, con
 // tokens 4.8 and 5.3, 4096 6.2 and 6.1, 8192 10.8 and 9.2 (and back 3.7 and
 // 4.4, 5.4 and 5.6, 7.5 and 7.2, 11.6 and 10.0).
 constexpr int kMany = 16, kFew = 4;
-bool few_tokens(int32_t T) { return T < 256 * kMany; }
+bool few_tokens(int32_t T, int32_t cus) { return T < cus * kMany; }
 
 template <int DH, int TYPE, int TG>
 hipError_t append_tg(const KvPages& kv, const int32_t* cu, const int32_t* len, int32_t T, const void* K, const void* V,
@@ -207,9 +207,9 @@ hipError_t append_tg(const KvPages& kv, const int32_t* cu, const int32_t* len, i
 }
 template <int DH, int TYPE>
 hipError_t append(const KvPages& kv, const int32_t* cu, const int32_t* len, int32_t T, const void* K, const void* V,
-                  hipStream_t stream) {
-  return few_tokens(T) ? append_tg<DH, TYPE, kFew>(kv, cu, len, T, K, V, stream)
-                       : append_tg<DH, TYPE, kMany>(kv, cu, len, T, K, V, stream);
+                  int32_t cus, hipStream_t stream) {
+  return few_tokens(T, cus) ? append_tg<DH, TYPE, kFew>(kv, cu, len, T, K, V, stream)
+                            : append_tg<DH, TYPE, kMany>(kv, cu, len, T, K, V, stream);
 }
 template <int DH, int TYPE, int TG>
 hipError_t read_tg(const KvPages& kv, const int32_t* cu, const int32_t* len, int32_t T, void* K, void* V, int32_t clear_rest,
@@ -220,9 +220,9 @@ hipError_t read_tg(const KvPages& kv, const int32_t* cu, const int32_t* len, int
 }
 template <int DH, int TYPE>
 hipError_t read(const KvPages& kv, const int32_t* cu, const int32_t* len, int32_t T, void* K, void* V, int32_t clear_rest,
-                hipStream_t stream) {
-  return few_tokens(T) ? read_tg<DH, TYPE, kFew>(kv, cu, len, T, K, V, clear_rest, stream)
-                       : read_tg<DH, TYPE, kMany>(kv, cu, len, T, K, V, clear_rest, stream);
+                int32_t cus, hipStream_t stream) {
+  return few_tokens(T, cus) ? read_tg<DH, TYPE, kFew>(kv, cu, len, T, K, V, clear_rest, stream)
+                            : read_tg<DH, TYPE, kMany>(kv, cu, len, T, K, V, clear_rest, stream);
 }
 
 }  // namespace
@@ -236,13 +236,13 @@ hipError_t read(const KvPages& kv, const int32_t* cu, const int32_t* len, int32_
   }
 
 hipError_t launch_kv_append(const KvPages& kv, const int32_t* cu, const int32_t* cache_len, int32_t T, const void* K,
-                            const void* V, hipStream_t stream) {
-  STARQ_KV_DISPATCH(append, kv, cu, cache_len, T, K, V, stream)
+                            const void* V, int32_t cus, hipStream_t stream) {
+  STARQ_KV_DISPATCH(append, kv, cu, cache_len, T, K, V, cus, stream)
 }
 
 hipError_t launch_kv_read(const KvPages& kv, const int32_t* cu, const int32_t* cache_len, int32_t T, void* K, void* V,
-                          int32_t clear_rest, hipStream_t stream) {
-  STARQ_KV_DISPATCH(read, kv, cu, cache_len, T, K, V, clear_rest, stream)
+                          int32_t clear_rest, int32_t cus, hipStream_t stream) {
+  STARQ_KV_DISPATCH(read, kv, cu, cache_len, T, K, V, clear_rest, cus, stream)
 }
 
 }  // namespace starq
