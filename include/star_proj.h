@@ -625,11 +625,13 @@ star_status star_attn_packed_bwd(const star_attn_shape *shape, const void *pack,
  *   type    STAR_KV_BF16, or 8 bits per element with a scale byte per row of a
  *           head, device uint8 [n_pages][n_kv_heads][page_size] for K and V
  *           each: STAR_KV_E4M3 (OCP e4m3) or STAR_KV_INT8.  A scale byte s
- *           stands for 2^(s - 127); a row's values are its elements times
- *           that.  s is the least (from 1 on) at which the row's largest
- *           magnitude fits the type (448, 127), elements are rounded to
- *           nearest even; a value read back is exact in bf16.  A row that
- *           holds a NaN or an infinity gets s = 255 and reads back as NaN.
+ *           from 1 to 254 stands for 2^(s - 127), 0 for zero; a row's values
+ *           are its elements times that.  s is the least (from 1 on) at which
+ *           the row's largest magnitude fits the type (448, 127), elements are
+ *           rounded to nearest even; a value read back is exact in bf16 (in
+ *           e4m3, magnitudes from 1.9375 2^127 on round to 2^128, which reads
+ *           back as infinity).  A row that holds a NaN or an infinity gets
+ *           s = 255 and elements of zero, and reads back as NaN.
  *   page_table  device int32 [batch][max_pages].  Entries behind a sequence's
  *           length are not read.  An entry outside [0, n_pages) is a page that
  *           is not there: its positions are neither written nor attended to
@@ -641,9 +643,9 @@ star_status star_attn_packed_bwd(const star_attn_shape *shape, const void *pack,
  * star_kv_append writes the rows K, V (device [T][n_kv_heads][head_dim], bf16)
  * of new tokens, packed by cu_seqlens (device int32[batch + 1]: a whole
  * prompt, one token each, none; bounds that cannot be count as for
- * star_attn_pack, so one array names the same rows to both), into the cache.  cache_len (device
- * int32[batch]) is every sequence's length with them, as star_attn_decode_paged
- * then takes it: token t of sequence b is position
+ * star_attn_pack, so one array names the same rows to both), into the cache.
+ * cache_len (device int32[batch]) is every sequence's length with them, as
+ * star_attn_decode_paged then takes it: token t of sequence b is position
  * cache_len[b] - (cu_seqlens[b + 1] - t).  Tokens whose position is below 0 or
  * beyond max_pages pages are left out.
  * star_kv_read is the inverse: the same arguments, K and V are written (rows

@@ -397,7 +397,8 @@ hipError_t launch_attn_decode(const AttnParams& p, hipStream_t stream);
 
 // Pages [n_pages][n_kv][page][head_dim] of bf16, e4m3 or int8; the 8-bit types
 // with a scale byte b per row of a head, [n_pages][n_kv][page]: the row's
-// values are its elements times 2^(b - 127), NaN for b = 255.  Position u of
+// values are its elements times 2^(b - 127), zeros for b = 0, NaN for b = 255 (and
+// elements of zero, as append writes them).  Position u of
 // sequence b lies in page table[b][u / page].
 enum KvType : int { kKvBf16 = 0, kKvE4m3 = 1, kKvInt8 = 2 };
 struct KvPages {

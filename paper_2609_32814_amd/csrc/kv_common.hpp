@@ -7,8 +7,9 @@ namespace starq {
 
 namespace {
 
-// 2^(b - 127) of scale byte e of a word.  Byte 255 is infinity, and a row that
-// has it holds zeros: every product with it is NaN, as the row's values are.
+// 2^(b - 127) of scale byte e of a word, zero for byte 0.  Byte 255 is infinity,
+// and a row that has it holds zeros: every product with it is NaN, as the row's
+// values are.
 __device__ __forceinline__ float kv_scale(uint32_t w, int e) {
   return __uint_as_float((e < 3 ? w << (23 - 8 * e) : w >> 1) & 0x7f800000u);
 }

@@ -91,3 +91,25 @@ def test_keys_some_of_which_weigh_nothing(P, cap, first):
                                  out_dtype=F32)
     rO, mag = ref.decode("dense", 1, t, lens, Q, [stored("bf16", x)[0] for x in K], [stored("bf16", x)[0] for x in V])
     assert ref.off(O, rO, (ref.HALF + ref.SLACK) * mag, False) <= 1
+
+
+@pytest.mark.parametrize("cap", [64, 4096])
+@pytest.mark.parametrize("kv", ["e4m3", "int8"])
+def test_scale_bytes_of_zero(P, kv, cap):
+    """Rows with scale byte 0 are zeros, whatever their elements: as after
+    clearing a cache's scales."""
+    H, Hkv, D, lens = 4, 2, 64, [40, 17]
+    K = [rnd((n, Hkv, D), 10 + b) for b, n in enumerate(lens)]
+    V = [rnd((n, Hkv, D), 20 + b) for b, n in enumerate(lens)]
+    c = filled(P, kv, K, V, lens, cap)
+    for b, u in ((0, 0), (0, 39), (1, 5), (1, 16)):
+        at = int(c.table[b, u // 16])
+        c.ks[at, :, u % 16], c.vs[at, 1, u % 16] = 0, 0
+        K[b][u], V[b][u, 1] = 0, 0
+    k64, v64 = [stored(kv, x)[0] for x in K], [stored(kv, x)[0] for x in V]
+    got = P.star_kv_read(c.pages, i32([0, 40, 57]), i32(lens), 57)
+    assert torch.equal(got[0].cpu().double(), torch.cat(k64)) and torch.equal(got[1].cpu().double(), torch.cat(v64))
+    Q, t = rnd((2, H, D), 5), ref.cyclic(cap, 4)
+    O = P.star_attn_decode_paged(P.AttnShape(2, cap, H, Hkv, D, 4), c.pages, t.to(DEV), i32(lens), Q.to(DEV), out_dtype=F32)
+    rO, mag = ref.decode("star", 4, t, lens, Q, k64, v64)
+    assert ref.off(O, rO, (ref.HALF + ref.SLACK) * mag, False) <= 1
