@@ -1747,7 +1747,7 @@ star_status parse_pages(const star_kv_pages* pg, KvPages& kv) {
 }
 // the pointers of a cache that is to be used
 star_status check_pages(const KvPages& kv) {
-  if (!kv.table && kv.max_pages > 0) return STAR_ERR_ARG;
+  if (!kv.table && kv.max_pages > 0 && kv.B > 0) return STAR_ERR_ARG;
   if (kv.n_pages > 0) {
     if (!kv.K || !kv.V) return STAR_ERR_ARG;
     if (kv.type != kKvBf16 && (!kv.k_scale || !kv.v_scale)) return STAR_ERR_ARG;
@@ -1762,7 +1762,7 @@ star_status check_rows(const KvPages& kv, int64_t T, const int32_t* cu, const in
   if (T < 0 || T > kKvMaxTokens) return STAR_ERR_SHAPE;
   if (kv.n_kv > (1 << 20)) return STAR_ERR_SHAPE;  // 16 n_kv rows of a workgroup are counted in 32 bits
   if (T == 0) return STAR_OK;
-  if (!cu || !cache_len || !K || !V) return STAR_ERR_ARG;
+  if (!cu || (!cache_len && kv.B > 0) || !K || !V) return STAR_ERR_ARG;
   if (!aligned4(cu) || !aligned4(cache_len) || !aligned16(K) || !aligned16(V)) return STAR_ERR_ALIGN;
   return check_pages(kv);
 }

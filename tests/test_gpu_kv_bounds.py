@@ -5,7 +5,7 @@ the same rows to every call."""
 import pytest
 import torch
 
-from test_gpu_paged import DEV, Cache, P, i32, rnd  # noqa: F401 (P: fixture)
+from test_gpu_paged import DEV, Cache, P, i32, rnd, stored  # noqa: F401 (P: fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -79,3 +79,36 @@ def test_many_sequences_with_bounds_out_of_order(P, B, T):
                 want[t] = K[t]
     for x in P.star_kv_read(c.pages, i32(cu), i32(length), T):
         assert torch.equal(x.cpu(), want)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+def test_no_sequence_at_all(P, kv):
+    """A cache of no sequences: every row is outside, none is written, all are
+    read back as zeros or left as they were."""
+    c = Cache(P, kv, 2, 64, 8, 0, 3)
+    before = [x.view(torch.uint8).clone() for x in (c.K, c.V)]
+    K = rnd((5, 2, 64), 1).to(DEV)
+    P.star_kv_append(c.pages, i32([0]), i32([]), K, K)
+    assert all(torch.equal(a, b.view(torch.uint8)) for a, b in zip(before, (c.K, c.V)))
+    assert not any(x.any() for x in P.star_kv_read(c.pages, i32([0]), i32([]), 5))
+    own = [torch.full_like(K, 5.0) for _ in range(2)]
+    P.star_kv_read(c.pages, i32([3]), i32([]), 5, *own)
+    assert all(bool((x == 5).all()) for x in own)
+    assert P.star_kv_read(c.pages, i32([0]), i32([]), 0)[0].shape == (0, 2, 64)
+    O = P.star_attn_decode_paged(P.AttnShape(0, 24, 2, 2, 64, 1), c.pages, i32([0] * 24), i32([]), K[:0])
+    assert O.shape == (0, 2, 64)
+
+
+def test_sequences_share_pages(P):
+    """Two sequences with one prompt's pages in both tables, going on in pages
+    of their own: each reads the whole of its own positions."""
+    D, Hkv, page = 64, 2, 8
+    c = Cache(P, "int8", Hkv, D, page, 2, 4)
+    c.dtable[1, :2] = c.dtable[0, :2]
+    K = [rnd((n, Hkv, D), 3 + k).to(DEV) for k, n in enumerate((16, 5, 9))]
+    P.star_kv_append(c.pages, i32([0, 16, 16]), i32([16, 0]), K[0], K[0])
+    P.star_kv_append(c.pages, i32([0, 5, 14]), i32([21, 25]), torch.cat(K[1:]), torch.cat(K[1:]))
+    got = P.star_kv_read(c.pages, i32([0, 21, 46]), i32([21, 25]), 46)
+    want = torch.cat([stored("int8", x.cpu())[0] for x in (K[0], K[1], K[0], K[2])])
+    for x in got:
+        assert torch.equal(x.cpu().double(), want)

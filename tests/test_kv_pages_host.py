@@ -44,3 +44,19 @@ def test_rows_that_no_launch_holds_are_refused():
         assert b.LIB.star_kv_read(ctypes.byref(pg), V(16), V(16), T, V(16), V(16), 1, 0, None) == shape
     assert b.LIB.star_kv_append(ctypes.byref(pg), V(16), V(16), top, None, V(16), 1, None) == arg
     assert b.LIB.star_kv_read(ctypes.byref(pg), V(16), V(16), top, None, V(16), 1, 0, None) == arg
+
+
+def test_no_sequence_at_all():
+    """A cache of no sequences has no table and no lengths: appending its
+    rows, which are outside every sequence, is done at once."""
+    import paper_2609_32814_amd as P
+
+    b, V = P.binding, ctypes.c_void_p
+    names = {v: k for k, v in b.STATUS_NAMES.items()}
+    none = b._CKvPages(10, 16, 2, 64, 0, 4, 1, 16, 16, 16, 16, None)
+    assert b.LIB.star_kv_append(ctypes.byref(none), V(16), None, 5, V(16), V(16), 1, None) == 0
+    assert b.LIB.star_kv_append(ctypes.byref(none), None, None, 5, V(16), V(16), 1, None) == names["STAR_ERR_ARG"]
+    one = b._CKvPages(10, 16, 2, 64, 1, 4, 1, 16, 16, 16, 16, 16)
+    assert b.LIB.star_kv_append(ctypes.byref(one), V(16), None, 5, V(16), V(16), 1, None) == names["STAR_ERR_ARG"]
+    one.page_table = None
+    assert b.LIB.star_kv_append(ctypes.byref(one), V(16), V(16), 5, V(16), V(16), 1, None) == names["STAR_ERR_ARG"]
