@@ -20,7 +20,7 @@ def P():
 
 def test_context(P, monkeypatch):
     on = P.binding._on
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(P.binding, "_current", lambda: 1)
     assert on(torch.device("cuda", 1)) is on(torch.device("cuda", 1))
     other = on(torch.device("cuda", 0))
     assert isinstance(other, torch.cuda.device) and other.idx == 0
