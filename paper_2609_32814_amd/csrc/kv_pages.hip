@@ -14,8 +14,8 @@
 // rows of one head's tokens side by side (they are neighbours in the page).  A
 // row's largest magnitude is joined by lane exchanges.  Both kernels are bound
 // by memory: every row is read once and written once.  40000 tokens, 8 heads of
-// 128, from e4m3: 59 us, 4.2 TB/s; 16411 tokens to e4m3 and back 19 us each
-// (in cache); 64 tokens: 3.8 us, a launch and the look-up of a page.
+// 128, from e4m3: 58 us, 4.3 TB/s; 16411 tokens to e4m3 and back 19 us each
+// (in cache); 64 tokens: 3.6 us, a launch and the look-up of a page.
 #include "attn_common.hpp"
 #include "kv_common.hpp"
 
@@ -32,7 +32,7 @@ constexpr int kThreads = 256;
 // a lane asked for at once, until one lies above all TG tokens; lane j ends
 // with the index of its first one above token t0 + j (INT32_MAX: none).  A
 // token each to int8, 12 heads of 64, us so and by halving: 64 sequences 3.6 and
-// 3.8, 4096 9.7 and 8.5, 16384 27 and 21.
+// 3.8, 4096 8.5 and 8.8, 16384 25.5 and 20.4.
 template <int TG>
 __device__ __forceinline__ int32_t first_above(const int32_t* cu, int32_t n_seq, int32_t t0, int lane, int wave) {
   int32_t first = INT32_MAX;
@@ -42,12 +42,18 @@ __device__ __forceinline__ int32_t first_above(const int32_t* cu, int32_t n_seq,
     for (int u = 0; u < 4; ++u) c[u] = k0 + 64 * u + lane <= n_seq ? cu[k0 + 64 * u + lane] : INT32_MIN;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      if (__ballot(c[u] > t0) == 0) continue;
+      const int32_t k = static_cast<int32_t>(k0) + 64 * u;
+      const uint64_t any = __ballot(c[u] > t0);
+      if (any == 0) continue;
+      const int at = __builtin_ctzll(any);
+      if (__builtin_amdgcn_readlane(c[u], at) > t0 + TG - 1) {  // one sequence holds them all
+        first = min(first, k + at);
+        continue;
+      }
 #pragma unroll
       for (int j = 0; j < TG; ++j) {
         const uint64_t m = __ballot(c[u] > t0 + j);
-        const int32_t at = m ? static_cast<int32_t>(k0) + 64 * u + __builtin_ctzll(m) : INT32_MAX;
-        if (lane == j) first = min(first, at);
+        if (lane == j) first = min(first, m ? k + __builtin_ctzll(m) : INT32_MAX);
       }
     }
     if (__ballot(lane < TG && first == INT32_MAX) == 0) break;
@@ -192,9 +198,9 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(const KvPages kv, con
 }
 
 // 16 tokens a workgroup; 4 where that would leave CUs without one.  To int8, 64
-// sequences, 12 heads of 64, us with 4 and with 16: 64 tokens 3.8 and 4.8, 2048
-// tokens 4.8 and 5.3, 4096 6.2 and 6.1, 8192 10.8 and 9.2 (and back 3.7 and
-// 4.4, 5.4 and 5.6, 7.5 and 7.2, 11.6 and 10.0).
+// sequences, 12 heads of 64, us with 4 and with 16: 64 tokens 3.6 and 4.9, 2048
+// tokens 4.6 and 5.1, 4096 6.0 and 6.3, 8192 10.1 and 9.1 (and back 3.6 and
+// 4.6, 5.2 and 5.5, 7.1 and 7.1, 10.6 and 10.2).
 constexpr int kMany = 16, kFew = 4;
 bool few_tokens(int32_t T, int32_t cus) { return T < cus * kMany; }
 
