@@ -23,8 +23,9 @@
 // TFLOP/s), 32 of 128 in 560 (982); the exponentials, conversions and sums of
 // 16 scores a lane bound the first (105 vector instructions a step, the VALU
 // busy 71 % of the time), the products the second.  24576 tokens in 17
-// sequences, 12 heads of 64, star law, q = 4: 221 to 250 us, by the same vector
-// work beside fewer products.  211 tokens in 3 sequences: 10 us, a launch and a
+// sequences, 12 heads of 64, star law, q = 4: 223 us in a long run, 250 to 274 in
+// short ones, by the same vector work beside fewer products (VALU busy 64 % of
+// the time, MFMA 22 %).  211 tokens in 3 sequences: 10 us, a launch and a
 // chain of dependent reads (plan, record, positions, rows), not bytes.
 #include <cfloat>
 #include <type_traits>
