@@ -894,7 +894,9 @@ def star_attn_pack_bytes(q: int, T: int, n_seq: int) -> int:
 def star_attn_pack(q: int, row_type: torch.Tensor, cu_seqlens: torch.Tensor, pack=None) -> torch.Tensor:
     """The plan of a pack (device uint8 buffer): sequence s is rows
     ``cu_seqlens[s]`` .. ``cu_seqlens[s + 1] - 1`` of types ``row_type`` [T].
-    Built once per batch; every layer's forward and backward take it."""
+    Built once per batch; every layer's forward and backward take it, for
+    shapes of that T, count of sequences and q (with others they write nothing,
+    outputs that they allocate included)."""
     dev = row_type.device
     T, n = row_type.numel(), cu_seqlens.numel() - 1
     _types(row_type, T, dev)

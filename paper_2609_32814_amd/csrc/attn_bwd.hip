@@ -28,10 +28,10 @@
 // Measured: one sequence of 8192, all features: dQ 830 us for 64 heads of 64
 // (990 TFLOP/s), 805 for 32 of 128 (1020); dK and dV 1105 (995) and 1105 (995),
 // bound by the products (a large library product reaches 1183).  24576 tokens
-// in 17 sequences, 12 heads of 64, star law, q = 4: 300 to 330 + 365 to 395 us; 8192
-// tokens in 6, 32 heads of 128 on 8, q = 2: 345 to 375 + 505 to 545.  1500 tokens: 21 + 21 us, a
-// prologue of about 8 us and up to 8 steps of 1 us, each a chain of reads,
-// products and exponentials that few wavefronts cannot hide.
+// in 17 sequences, 12 heads of 64, star law, q = 4: 300 to 330 + 365 to 395 us;
+// 8192 tokens in 6, 32 heads of 128 on 8, q = 2: 345 to 375 + 505 to 545.  1500
+// tokens: 21 + 21 us, a prologue of about 8 us and up to 8 steps of 1 us, each a
+// chain of reads, products and exponentials that few wavefronts cannot hide.
 #include <type_traits>
 
 #include "attn_common.hpp"
